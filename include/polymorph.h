@@ -367,6 +367,120 @@ int pm_layernorm(const void* x, const float* gamma, const float* beta, void* y,
 int pm_attention(const void* qkv, void* out, int n_frames, int tokens, int heads, int dtype,
                  void* cuda_stream);
 
+/* ---- encoders that pack sequences of different lengths ----------------------------------- */
+/* (The paper has no counterpart: its frames are all of one size and its positions a learned table.  These operators serve
+ * encoders over the same streams whose cameras differ in size, whose blocks rotate queries and keys by position, or whose new
+ * frames attend to what a stream has kept.)  Inference only: there is no backward pass in this library.
+ *
+ * A matrix of heads is [rows, heads, head_dim] with any distance between rows (given in elements, a multiple of 16 bytes, at least
+ * heads * head_dim) and the heads of a row side by side; its address is 16-byte aligned.  So queries, keys and values may be
+ * column ranges of one qkv projection.  All calls are asynchronous, allocate nothing and can be captured in a CUDA graph; the
+ * stream must belong to the current device, or be one of the default streams (else PM_ERR_ARG). */
+
+#define PM_ROPE_MAX_DIM 256
+#define PM_ROPE_MAX_HEADS 1024
+
+/* How frequencies are scaled for positions beyond the trained length. */
+enum {
+    PM_ROPE_PLAIN = 0,
+    PM_ROPE_LINEAR = 1,     /* every frequency / factor                                                   */
+    PM_ROPE_NTK = 2,        /* base * factor^(p / (p - 1)), p pairs per axis: the last pair is slowed by factor, the first kept */
+    PM_ROPE_BANDS = 3       /* by the number of turns over `original` positions: at least high_turns kept, at most low_turns
+                               / factor, in between in proportion                                          */
+};
+
+/* Rotation by position: pair i of the first rot_dim dimensions of a head turns by position * frequency.  axes = 1: one position
+ * per row, frequency base^(-i / (rot_dim / 2)); axes = 2: two positions per row (row and column of a patch, say), the first half of the
+ * pairs turns by the first, the second half by the second, frequencies base^(-j / (rot_dim / 4)) for the j-th pair of either. */
+typedef struct {
+    int head_dim;           /* multiple of 16, at most PM_ROPE_MAX_DIM                                   */
+    int rot_dim;            /* multiple of 16, at most head_dim; dimensions behind it pass unchanged     */
+    int interleaved;        /* pair i is dimensions (2 i, 2 i + 1); else (i, i + rot_dim / 2)             */
+    int axes;               /* 1 or 2                                                                    */
+    int scaling;            /* PM_ROPE_*                                                                 */
+    float amplitude;        /* cos and sin are multiplied by it (1 = a rotation)                         */
+    double base;            /* > 0, finite                                                               */
+    double factor;          /* > 0; read unless PM_ROPE_PLAIN                                            */
+    double original, low_turns, high_turns;      /* read for PM_ROPE_BANDS: > 0, low_turns < high_turns  */
+} pm_rope_config;
+
+/* What the calls below take: filled by pm_rope_init on the host, plain data, copied by each call.  step[i] is pair i's
+ * turns per position in units of 2^-64 turns, so angles of any 32-bit position are exact to 2^-33 turns. */
+typedef struct {
+    int head_dim, rot_dim, interleaved, axes;
+    float amplitude;
+    int reserved;
+    unsigned long long step[PM_ROPE_MAX_DIM / 2];
+} pm_rope_table;
+
+/* Host function; needs no GPU.  Errors: PM_ERR_ARG (NULL, a value out of the ranges above, frequencies that overflow),
+ * PM_ERR_CAPACITY (head_dim > PM_ROPE_MAX_DIM). */
+int pm_rope_init(const pm_rope_config* cfg, pm_rope_table* out);
+
+/* Rotates the heads of each row by the row's position.
+ *   x dev [rows, heads, head_dim], y dev the same shape (bf16 or fp32 per dtype); y may be x itself (same address and distance
+ *     between rows); otherwise they must not overlap
+ *   positions  dev int32 [rows, axes], any value
+ * Errors: PM_ERR_ARG, PM_ERR_CAPACITY (heads > PM_ROPE_MAX_HEADS), PM_ERR_CUDA. */
+int pm_rope(const void* x, long long x_stride, void* y, long long y_stride, const int32_t* positions, int rows, int heads,
+            const pm_rope_table* table, int dtype, void* cuda_stream);
+
+enum { PM_NORM_RMS = 0, PM_NORM_LAYER = 1 };
+
+/* A norm of every query and key head by itself and, in the same pass, the rotation by position:
+ *   RMS    u = x * gamma / sqrt(mean(x^2) + eps)          LAYER  u = (x - mean) * gamma / sqrt(var + eps) + beta   (biased variance)
+ * over the head_dim elements of a head, in fp32; then y = rotation of u (table NULL: y = u). */
+typedef struct {
+    const void *q, *k;                    /* dev [rows, heads, head_dim], [rows, kv_heads, head_dim]          */
+    void *q_out, *k_out;                  /* dev, the same shapes; each may be its input itself                */
+    long long q_stride, k_stride, q_out_stride, k_out_stride;     /* elements between rows                   */
+    const float *q_gamma, *k_gamma;       /* dev fp32 [head_dim], 16-byte aligned, or with per_head [heads, head_dim] and [kv_heads, head_dim] */
+    const float *q_beta, *k_beta;         /* dev fp32 as gamma, or NULL; LAYER only                            */
+    const int32_t* positions;             /* dev int32 [rows, axes]; read if table is given                    */
+    const pm_rope_table* table;           /* host, or NULL: no rotation                                        */
+    int rows, heads, kv_heads, head_dim;  /* kv_heads = 0: queries only (k, k_out, k_gamma unused); head_dim multiple of 16 */
+    int norm, per_head;
+    float eps;                            /* >= 0                                                              */
+    int dtype;
+} pm_qk_norm_rope_args;
+
+/* Errors: PM_ERR_ARG, PM_ERR_CAPACITY (head_dim > PM_ROPE_MAX_DIM, heads > PM_ROPE_MAX_HEADS), PM_ERR_CUDA. */
+int pm_qk_norm_rope(const pm_qk_norm_rope_args* args, void* cuda_stream);
+
+/* Attention over packed sequences: sequence s has the queries of rows q_offsets[s] .. q_offsets[s + 1] - 1 and the keys and values
+ * of rows kv_offsets[s] .. + its number of keys; query head h reads K/V head h / (heads / kv_heads):
+ *   out[j, h] = sum_{t < vis} softmax_{t < vis}(scale q[j, h] . k[t]) v[t]
+ *   vis = n_k, or with `causal` clamp(j + 1 + n_k - n_q, 0, n_k): the last query sees all keys (n_q, n_k the sequence's numbers
+ *   of queries and keys).  A query that sees nothing gives zeros.
+ * New frames or single tokens of a stream attend to what it has kept in this form too: n_q new queries, n_k = kept + n_q.
+ * Rows of q, k, v and out that belong to no sequence are neither used nor written.  Within a sequence, keys that causal order
+ * hides from a query may hold anything; values must be finite (a hidden one takes part with weight zero). */
+typedef struct {
+    const void *q, *k, *v;                /* dev [q_rows, heads, head_dim], [kv_rows, kv_heads, head_dim] twice; 16-byte aligned */
+    void* out;                            /* dev [q_rows, heads, head_dim]; overlaps no input                  */
+    long long q_stride, k_stride, v_stride, out_stride;           /* elements between rows                   */
+    const int32_t* q_offsets;             /* dev int32 [n_seqs + 1], ascending                                 */
+    const int32_t* kv_offsets;            /* dev int32 [n_seqs + 1], or [n_seqs] with kv_lengths; NULL: q_offsets */
+    const int32_t* kv_lengths;            /* dev int32 [n_seqs]: number of keys of each sequence (slots of a cache); NULL: kv_offsets[s + 1] - kv_offsets[s] */
+    int q_rows, kv_rows;                  /* rows of the buffers                                               */
+    int n_seqs;                           /* at most PM_PACKED_MAX_SEQS                                        */
+    int max_q, max_kv;                    /* no sequence has more queries, keys than this                      */
+    int heads, kv_heads;                  /* heads a multiple of kv_heads, at most PM_PACKED_MAX_GROUP times   */
+    int head_dim;                         /* 64 or 128                                                         */
+    int causal;
+    float scale;                          /* > 0, or 0 for 1 / sqrt(head_dim)                                  */
+    int dtype;                            /* 0 = bf16 tensor-core kernels, 1 = fp32                            */
+    int32_t* status_out;                  /* dev int32 or NULL: cleared by the call; PM_ERR_ARG if a sequence's offsets or length are
+                                             malformed, lie outside the buffers or exceed max_q / max_kv (the sequence is skipped, its
+                                             rows of out left as they were), PM_ERR_TIMEOUT if a bounded wait expired */
+} pm_packed_attention;
+
+#define PM_PACKED_MAX_SEQS 4096
+#define PM_PACKED_MAX_GROUP 64
+/* Errors: PM_ERR_ARG (NULL, ranges, alignment), PM_ERR_CAPACITY (n_seqs, heads / kv_heads, kv_heads > 65535, max_q * heads / kv_heads >= 2^30),
+ * PM_ERR_CUDA.  Nothing is launched on error. */
+int pm_attention_packed(const pm_packed_attention* args, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

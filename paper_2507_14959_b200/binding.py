@@ -24,6 +24,7 @@ EXPORTS = [
     "pm_select_static", "pm_metrics_reset", "pm_metrics_read", "pm_status", "pm_last_error", "pm_launch_count", "pm_set_graphs", "pm_set_small_batch_kernel", "pm_profile_enable", "pm_profile_read", "pm_plan_stats", "pm_linear_create", "pm_linear_register",
     "pm_linear_forward", "pm_linear_status", "pm_linear_last_error", "pm_linear_destroy",
     "pm_layernorm", "pm_attention", "pm_selftest_wait_timeout", "pm_linear_kernel", "pm_cooccurrence", "pm_build_contexts", "pm_intra_coherence",
+    "pm_rope_init", "pm_rope", "pm_qk_norm_rope", "pm_attention_packed",
 ]
 
 
@@ -54,6 +55,38 @@ class pm_adapter(C.Structure):
     _fields_ = [("rank", C.c_int), ("scale", C.c_float), ("A", C.POINTER(_FP)), ("B", C.POINTER(_FP)),
                 ("n_cls", C.c_int), ("class_ids", C.POINTER(C.c_int32)), ("head_w", _FP),
                 ("head_b", _FP), ("acc", _FP)]
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3}
+NORMS = {"rms": 0, "layer": 1}
+ROPE_MAX_DIM = 256
+
+
+class pm_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int), ("rot_dim", C.c_int), ("interleaved", C.c_int), ("axes", C.c_int), ("scaling", C.c_int),
+                ("amplitude", C.c_float), ("base", C.c_double), ("factor", C.c_double), ("original", C.c_double),
+                ("low_turns", C.c_double), ("high_turns", C.c_double)]
+
+
+class pm_rope_table(C.Structure):
+    _fields_ = [("head_dim", C.c_int), ("rot_dim", C.c_int), ("interleaved", C.c_int), ("axes", C.c_int), ("amplitude", C.c_float),
+                ("reserved", C.c_int), ("step", C.c_ulonglong * (ROPE_MAX_DIM // 2))]
+
+
+class pm_qk_norm_rope_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "q_out", "k_out")] +
+                [(n, C.c_longlong) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")] +
+                [(n, C.c_void_p) for n in ("q_gamma", "k_gamma", "q_beta", "k_beta", "positions", "table")] +
+                [(n, C.c_int) for n in ("rows", "heads", "kv_heads", "head_dim", "norm", "per_head")] +
+                [("eps", C.c_float), ("dtype", C.c_int)])
+
+
+class pm_packed_attention(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "v", "out")] +
+                [(n, C.c_longlong) for n in ("q_stride", "k_stride", "v_stride", "out_stride")] +
+                [(n, C.c_void_p) for n in ("q_offsets", "kv_offsets", "kv_lengths")] +
+                [(n, C.c_int) for n in ("q_rows", "kv_rows", "n_seqs", "max_q", "max_kv", "heads", "kv_heads", "head_dim", "causal")] +
+                [("scale", C.c_float), ("dtype", C.c_int), ("status_out", C.c_void_p)])
 
 
 _lib = None
@@ -106,6 +139,10 @@ def load():
     lib.pm_attention.argtypes = [vp, vp, ip, ip, ip, ip, vp]
     lib.pm_selftest_wait_timeout.argtypes = [C.c_longlong, vp, vp, vp]
     lib.pm_linear_kernel.argtypes = [ip, ip, ip, ip, ip, ip, C.POINTER(C.c_int32)]
+    lib.pm_rope_init.argtypes = [C.POINTER(pm_rope_config), C.POINTER(pm_rope_table)]
+    lib.pm_rope.argtypes = [vp, C.c_longlong, vp, C.c_longlong, vp, ip, ip, vp, ip, vp]
+    lib.pm_qk_norm_rope.argtypes = [vp, vp]
+    lib.pm_attention_packed.argtypes = [vp, vp]
     _lib = lib
     return lib
 
@@ -435,3 +472,134 @@ def intra_coherence(contexts, co_norm):
     if rc != PM_OK:
         raise PolymorphError(rc, "pm_intra_coherence")
     return out.value
+
+
+# ---- encoders that pack sequences of different lengths ----------------------------------------------
+def _here(where, dtype_name, *tensors):
+    """Refuses tensors of another element type, on the host or on another device than the current one."""
+    import torch
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for name, t, want in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or t.get_device() != here:
+            raise PolymorphError(PM_ERR_ARG, where, f"{name} is not on the current device")
+        if t.dtype != (getattr(torch, dtype_name) if want is None else getattr(torch, want)):
+            raise PolymorphError(PM_ERR_ARG, where, f"{name} has type {t.dtype}")
+
+
+def _heads(where, name, t):
+    """(rows, heads, head_dim, elements between rows) of [rows, heads, head_dim] whose heads lie side by side in a row."""
+    if t.dim() != 3:
+        raise PolymorphError(PM_ERR_ARG, where, f"{name} is not [rows, heads, head_dim]")
+    (rows, heads, dim), (row, head, element) = t.shape, t.stride()
+    if (dim > 1 and element != 1) or (heads > 1 and head != dim):
+        raise PolymorphError(PM_ERR_ARG, where, f"the heads of a row of {name} do not lie side by side")
+    return rows, heads, dim, row if rows > 1 else max(row, heads * dim)
+
+
+def _ints_of(where, name, t, *shapes):
+    """Refuses an index tensor that is not contiguous or has none of the shapes."""
+    if not t.is_contiguous() or tuple(t.shape) not in shapes:
+        raise PolymorphError(PM_ERR_ARG, where, f"{name} has shape {tuple(t.shape)} or is not contiguous")
+
+
+def _type_name(where, dtype):
+    if dtype not in (0, 1):
+        raise PolymorphError(PM_ERR_ARG, where, "dtype is 0 (bf16) or 1 (fp32)")
+    return "bfloat16" if dtype == 0 else "float32"
+
+
+class RopeTable:
+    """pm_rope_init: rotation by position for heads of head_dim, kept by the caller and passed to rope() and qk_norm_rope()."""
+
+    def __init__(self, head_dim, *, rot_dim=None, base=10000.0, interleaved=False, axes=1, scaling="none", factor=1.0, original=0.0,
+                 low_turns=1.0, high_turns=4.0, amplitude=1.0):
+        if scaling not in ROPE_SCALINGS:
+            raise PolymorphError(PM_ERR_ARG, "pm_rope_init", f"scaling is one of {', '.join(ROPE_SCALINGS)}")
+        cfg = pm_rope_config(head_dim, head_dim if rot_dim is None else rot_dim, int(bool(interleaved)), axes, ROPE_SCALINGS[scaling], amplitude,
+                             base, factor, original, low_turns, high_turns)
+        self.table = pm_rope_table()
+        rc = load().pm_rope_init(C.byref(cfg), C.byref(self.table))
+        if rc != PM_OK:
+            raise PolymorphError(rc, "pm_rope_init")
+        self.head_dim, self.axes, self.address = head_dim, axes, C.addressof(self.table)
+
+
+def _positions(where, positions, rows, axes):
+    _ints_of(where, "positions", positions, *([(rows,), (rows, 1)] if axes == 1 else [(rows, axes)]))
+
+
+def rope(x, y, positions, table, dtype, stream=None):
+    """pm_rope: x, y = torch CUDA [rows, heads, head_dim] (y may be x), positions = torch CUDA int32 [rows] or [rows, 2]."""
+    lib, where = load(), "pm_rope"
+    name = _type_name(where, dtype)
+    _here(where, name, ("x", x, None), ("y", y, None), ("positions", positions, "int32"))
+    rows, heads, dim, xs = _heads(where, "x", x)
+    ys = _heads(where, "y", y)[3]
+    if y.shape != x.shape or dim != table.head_dim:
+        raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
+    _positions(where, positions, rows, table.axes)
+    rc = lib.pm_rope(_ptr(x), xs, _ptr(y), ys, _ptr(positions), rows, heads, table.address, dtype, _stream_ptr(stream))
+    if rc != PM_OK:
+        raise PolymorphError(rc, where)
+
+
+def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_beta=None, k_beta=None, positions=None, table=None, stream=None):
+    """pm_qk_norm_rope: q, k and their outputs = torch CUDA [rows, heads, head_dim] (an output may be its input; k may be None);
+    gamma, beta = torch CUDA fp32 [head_dim], or [heads, head_dim] for weights of each head; norm "rms" or "layer"."""
+    lib, where = load(), "pm_qk_norm_rope"
+    name = _type_name(where, dtype)
+    if norm not in NORMS:
+        raise PolymorphError(PM_ERR_ARG, where, "norm is rms or layer")
+    if (table is None) != (positions is None):
+        raise PolymorphError(PM_ERR_ARG, where, "positions and table go together")
+    _here(where, name, ("q", q, None), ("k", k, None), ("q_out", q_out, None), ("k_out", k_out, None), ("positions", positions, "int32"),
+          *((n, t, "float32") for n, t in (("q_gamma", q_gamma), ("k_gamma", k_gamma), ("q_beta", q_beta), ("k_beta", k_beta))))
+    rows, heads, dim, qs = _heads(where, "q", q)
+    qos = _heads(where, "q_out", q_out)[3]
+    kv_heads = ks = kos = 0
+    if k is not None:
+        _, kv_heads, _, ks = _heads(where, "k", k)
+        kos = _heads(where, "k_out", k_out)[3]
+        if k.shape != (rows, kv_heads, dim) or k_out.shape != k.shape:
+            raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
+    if q_out.shape != q.shape or (table is not None and dim != table.head_dim):
+        raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
+    per_head = q_gamma.dim() == 2
+    for n, t, h in (("q_gamma", q_gamma, heads), ("q_beta", q_beta, heads), ("k_gamma", k_gamma, kv_heads), ("k_beta", k_beta, kv_heads)):
+        if t is not None:
+            _ints_of(where, n, t, (h, dim) if per_head else (dim,))
+    if table is not None:
+        _positions(where, positions, rows, table.axes)
+    args = pm_qk_norm_rope_args(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), qs, ks, qos, kos, _ptr(q_gamma), _ptr(k_gamma), _ptr(q_beta), _ptr(k_beta),
+                                _ptr(positions), None if table is None else table.address, rows, heads, kv_heads, dim, NORMS[norm], int(per_head), eps, dtype)
+    rc = lib.pm_qk_norm_rope(C.byref(args), _stream_ptr(stream))
+    if rc != PM_OK:
+        raise PolymorphError(rc, where)
+
+
+def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offsets=None, kv_lengths=None, causal=False, scale=None, status=None,
+                     stream=None):
+    """pm_attention_packed: q, out = torch CUDA [rows, heads, head_dim], k, v = [kv rows, kv_heads, head_dim]; q_offsets = torch CUDA int32
+    [n + 1]; kv_offsets = the same for keys ([n] suffices with kv_lengths = [n]); status = torch CUDA int32 [1] or None."""
+    lib, where = load(), "pm_attention_packed"
+    name = _type_name(where, dtype)
+    _here(where, name, ("q", q, None), ("k", k, None), ("v", v, None), ("out", out, None),
+          *((n, t, "int32") for n, t in (("q_offsets", q_offsets), ("kv_offsets", kv_offsets), ("kv_lengths", kv_lengths), ("status", status))))
+    rows, heads, dim, qs = _heads(where, "q", q)
+    kv_rows, kv_heads, _, ks = _heads(where, "k", k)
+    vs, os_ = _heads(where, "v", v)[3], _heads(where, "out", out)[3]
+    if k.shape != v.shape or out.shape != q.shape or k.shape[2] != dim:
+        raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
+    n = q_offsets.numel() - 1
+    _ints_of(where, "q_offsets", q_offsets, (n + 1,))
+    if kv_offsets is not None:
+        _ints_of(where, "kv_offsets", kv_offsets, (n + 1,), *([(n,)] if kv_lengths is not None else []))
+    if kv_lengths is not None:
+        _ints_of(where, "kv_lengths", kv_lengths, (n,))
+    args = pm_packed_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(out), qs, ks, vs, os_, _ptr(q_offsets), _ptr(kv_offsets), _ptr(kv_lengths), rows, kv_rows, n,
+                               int(max_q), int(max_kv), heads, kv_heads, dim, int(bool(causal)), 0.0 if scale is None else scale, dtype, _ptr(status))
+    rc = lib.pm_attention_packed(C.byref(args), _stream_ptr(stream))
+    if rc != PM_OK:
+        raise PolymorphError(rc, where)

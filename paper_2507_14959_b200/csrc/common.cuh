@@ -220,6 +220,19 @@ cudaError_t launch_select(const Launch& L, const float* scores, int n_frames, in
                           int* next_off, int* next_ids, int ids_capacity,
                           unsigned long long* metrics = nullptr);   // [frames, sum |S_t|, switches] or null
 
+// The current device, for an operator without a handle: a stream of another device is refused.
+inline int stream_device(cudaStream_t st, int* dev) {
+    if (cudaGetDevice(dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (st == nullptr || st == cudaStreamLegacy || st == cudaStreamPerThread) return PM_OK;
+    // a capture would be invalidated by the question; there, a launch into another device's stream fails by itself
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &capture) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (capture != cudaStreamCaptureStatusNone) return PM_OK;
+    int of = -1;
+    if (cudaStreamGetDevice(st, &of) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    return of == *dev ? PM_OK : PM_ERR_ARG;
+}
+
 // cudaFuncSetAttribute acts on the current device only, so "already set" is remembered per device
 // ordinal: the largest dynamic shared-memory size granted to one kernel on each device.
 struct SmemGrant {
