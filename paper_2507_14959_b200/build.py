@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpolymorph.so")
 SOURCES = ["api.cu", "kernels_simple.cu", "gemm_tcgen05.cu", "small_linear.cu", "shrink.cu", "attention.cu", "plan_device.cu", "contexts.cu", "latency_kernel.cu",
-           "rotary.cu", "attention_packed.cu"]
+           "rotary.cu", "attention_packed.cu", "attention_packed_tc.cu"]
 
 
 def nvcc_path() -> str:

@@ -1,7 +1,8 @@
 // Attention over packed sequences (pm_attention_packed):  out[j] = sum_{t < vis(j)} softmax(scale q[j].k[t]) v[t]  per query head.
 //
 // The rows of a (sequence, K/V head) pair are its (query, head of the group) pairs, row r = query r / group, head r % group, so
-// keys and values are read once for all heads that share them.  Two kernels:
+// keys and values are read once for all heads that share them.  Three kernels: attention_packed_tc_kernel (tcgen05, tiles of 256
+// rows; attention_packed_tc.cu), and here
 //   attention_rows_kernel   few rows (single tokens, short sequences): 16 rows per CTA, the keys split among warps and CTAs
 //   attention_f32_kernel    fp32 on CUDA cores
 // Both keep the running maximum m, sum l and unnormalised output O of a row in fp32 while they pass over the keys once, and join
@@ -493,6 +494,8 @@ cudaError_t launch_f32(const Launch& L, const PackedArgs& a, int n_sms) {
     return e;
 }
 
+constexpr int PACKED_FEW_ROWS = 64;          // rows of a (sequence, K/V head) pair up to which 16-row tiles serve
+
 bool heads_ok(const void* p, long long stride, int heads, int dim, int dtype) {
     return p && ((uintptr_t)p & 15) == 0 && stride >= (long long)heads * dim && stride % (dtype == 0 ? 8 : 4) == 0;
 }
@@ -543,6 +546,8 @@ extern "C" int pm_attention_packed(const pm_packed_attention* p, void* cuda_stre
         const bool few = (long long)a.max_q * a.group <= 16;
         e = p->head_dim == 64 ? (few ? launch_f32<64, 16>(L, a, n_sms) : launch_f32<64, 64>(L, a, n_sms))
                               : (few ? launch_f32<128, 16>(L, a, n_sms) : launch_f32<128, 64>(L, a, n_sms));
+    } else if (a.kv_rows > 0 && (long long)a.max_q * a.group > PACKED_FEW_ROWS) {
+        e = launch_packed_tc(L, a, p->head_dim, n_sms);
     } else {
         e = p->head_dim == 64 ? launch_rows<64>(L, a, n_sms) : launch_rows<128>(L, a, n_sms);
     }

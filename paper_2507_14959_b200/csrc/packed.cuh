@@ -16,6 +16,9 @@ struct PackedArgs {
 };
 
 
+// the tcgen05 kernel (attention_packed_tc.cu); a.kv_rows > 0
+cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim, int n_sms);
+
 namespace {
 
 struct Segment { int q0, nq, k0, nk; };
