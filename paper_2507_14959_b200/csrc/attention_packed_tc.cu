@@ -1,23 +1,26 @@
 // Attention over packed sequences on the tcgen05 tensor cores (bf16; the operator is described in attention_packed.cu).
 //
-// One persistent CTA per SM walks units: two tiles of 128 rows of a (sequence, K/V head) pair -- a row is a (query, head of the group) pair,
-// so a tile holds TT = 128 / group queries of all the heads that share K and V, and the keys and values of a block serve 256 rows.  Key
-// blocks of 128 pass through a ring in shared memory.  Per tile and block
-//     S = Q K^T             UMMA 128 x 128 x 16 steps, fp32 scores in tensor memory
-//     P = 2^(c S - c m)     one row per thread: the row's scores in registers, written back as packed bf16
+// A persistent CTA (two per SM for head dim 64) walks units: two tiles of 128 rows of a (sequence, K/V head) pair -- a row is a (query,
+// head of the group) pair, so a tile holds TT = 128 / group queries of all the heads that share K and V, and the keys and values of
+// a block serve 256 rows.  Key blocks of 64 pass through a ring in shared memory.  Per tile and block
+//     S = Q K^T             UMMA 128 x 64 x 16 steps, fp32 scores in tensor memory
+//     P = 2^(c S - c m)     one row per thread: its 64 scores in registers, written back over S as packed bf16
 //     O += P V              UMMA 128 x D x 16 steps, P read from tensor memory, V as an MN-major operand
+//     out = O / sum         after the last block, by the same threads
 // m is the row's running maximum, but it only moves when it has grown by more than 2^8 in the exponential's scale: then the thread
 // takes its row of O and of the sum down to the new one (no overflow can come of the lag: terms stay below 2^8, sums below 2^8 n).
-//     warps 0..3, 4..7    softmax of the two tiles
-//     warps 8..11         output of both: O / sum to global memory, while the softmax is at the next unit
-//     warp 12             MMA issue: the scores of step g + 1 before or right after the products of step g
-//     warp 13             units, TMA loads
-//     warp 14             the rows of a value block that lie behind the sequence's last key are set to zero (at most 15 of them
+//     warps 0..3, 4..7    softmax and output of the two tiles
+//     warp 8              MMA issue
+//     warp 9              units, TMA loads
+//     warp 10             the rows of a value block that lie behind the sequence's last key are set to zero (at most 15 of them
 //                         take part in a product, with weight zero; what lies there may be NaN)
-// Scores of head dim 64 have tensor memory of their own beside P, so the next block's are formed while this one's
-// exponentials run; with 128 P lies over S and the two tiles take turns.
+// What bounds it is a tile's chain of dependent steps -- wait, load, maximum, exponentials, store, signal, product, scores -- of which the
+// special-function unit, the next limit, sees a third.  So several tiles take turns on an SM: with head dim 64 two CTAs of two tiles each
+// (half of tensor memory: 64 columns of S and 64 of O a tile), with 128 one CTA whose tiles have two buffers of S, so that
+// the next scores are formed meanwhile.
 // Units are visited from the last rows of the sequences to the first, so in causal order the long ones come first.
 #include <algorithm>
+#include <type_traits>
 
 #include "f32x2.cuh"
 #include "packed.cuh"
@@ -26,25 +29,23 @@
 
 namespace {
 
-constexpr int PT_THREADS = 512;
+constexpr int PT_SOFTMAX = 4;                                 // softmax warps of a tile
+constexpr int PT_THREADS = 32 * (2 * PT_SOFTMAX + 4);
 constexpr int PT_ROWS = 128;                                  // rows of a tile
-constexpr int PT_KEYS = 128;                                  // keys of a block
+constexpr int PT_KEYS = 64;                                   // keys of a block
 constexpr int PT_UNITS = 4;                                   // units announced ahead
-constexpr int PT_TAILS = 2 * PT_UNITS;                        // barriers of value blocks to be cleared; the loads are at most PT_UNITS units ahead of warp 14
+constexpr int PT_TAILS = 2 * PT_UNITS;                        // barriers of value blocks to be cleared; the loads are at most PT_UNITS units ahead of warp 10
+constexpr int PT_POLY = 2;                                    // of eight pairs of exponentials, those worked out by ex2_poly
 constexpr float PT_LAG = 8.f;                                 // log2 of how far a row's terms may exceed 1
-// registers per thread of the warpgroups; their sum is what the launch brings (512 threads x 128)
-constexpr int PT_REGS_SOFTMAX = 200, PT_REGS_OUT = 64, PT_REGS_ISSUE = 48;
-static_assert(2 * PT_REGS_SOFTMAX + PT_REGS_OUT + PT_REGS_ISSUE <= 4 * 128, "register shares");
 
 template <int D>
 struct PtLayout {
-    static constexpr bool OWN_P = D == 64;                    // P beside S: the next scores need not wait for the product
-    static constexpr int SLOT = 128 * D * 2;                  // bytes of a Q tile, a K block, a V block
-    static constexpr int Q_SLOTS = 3, KV_SLOTS = D == 64 ? 8 : 4;
-    static constexpr int SUMS = OWN_P ? 4 : 2;                // buffers of row sums (see the softmax warps)
-    static __host__ __device__ constexpr uint32_t s_col(int i) { return OWN_P ? i * 256 : i * 128; }
-    static __host__ __device__ constexpr uint32_t p_col(int i) { return OWN_P ? i * 256 + 128 : i * 128; }
-    static __host__ __device__ constexpr uint32_t o_col(int i) { return OWN_P ? i * 256 + 192 : 256 + i * 128; }
+    static constexpr uint32_t TMEM = 512;
+    static constexpr int Q_BYTES = PT_ROWS * D * 2, KV_BYTES = PT_KEYS * D * 2;       // of a tile's queries, of a K or V block
+    static constexpr int Q_SLOTS = D == 64 ? 4 : 3, KV_SLOTS = D == 64 ? 12 : 8;
+    // a tile's columns: two buffers of scores, O
+    static __host__ __device__ constexpr uint32_t s_col(int i, uint32_t buffer) { return i * 256 + buffer * PT_KEYS; }
+    static __host__ __device__ constexpr uint32_t o_col(int i) { return i * 256 + 2 * PT_KEYS; }
 };
 
 struct PtUnit {                                               // 32 bytes
@@ -54,18 +55,18 @@ struct PtUnit {                                               // 32 bytes
 
 template <int D>
 struct PtControl {
-    float sums[PtLayout<D>::SUMS][2][PT_ROWS];
     PtUnit units[PT_UNITS];
     unsigned long long q_full[PtLayout<D>::Q_SLOTS], q_empty[PtLayout<D>::Q_SLOTS];
     unsigned long long kv_full[PtLayout<D>::KV_SLOTS], kv_empty[PtLayout<D>::KV_SLOTS];
-    unsigned long long s_ready[2], s_read[2], p_ready[2], pv_done[2], o_ready[2], o_read[2], l_ready[2];
+    // a buffer of scores each: a wait tells one phase from the next, not from the one after, and both sides may be a step ahead
+    unsigned long long s_ready[2][2], p_ready[2][2], pv_done[2], o_ready[2];
     unsigned long long tail[PT_TAILS], unit_full[PT_UNITS], unit_empty[PT_UNITS];
     uint32_t tmem;
     int abort;
 };
 template <int D>
 __host__ __device__ constexpr size_t pt_smem() {
-    return (size_t)(PtLayout<D>::Q_SLOTS + PtLayout<D>::KV_SLOTS) * PtLayout<D>::SLOT + sizeof(PtControl<D>);
+    return (size_t)PtLayout<D>::Q_SLOTS * PtLayout<D>::Q_BYTES + (size_t)PtLayout<D>::KV_SLOTS * PtLayout<D>::KV_BYTES + sizeof(PtControl<D>);
 }
 static_assert(pt_smem<64>() <= 227 * 1024 && pt_smem<128>() <= 227 * 1024, "shared memory");
 
@@ -74,24 +75,79 @@ struct PtArgs {
     int tile_tokens;                                          // TT
 };
 
-template <int N>
-__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// Bounded wait in which the hardware lets the warp sleep.
+__device__ __forceinline__ uint32_t try_wait_asleep(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(20000u)                  // ns
+        : "memory");
+    return ok;
+}
+__device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
+    if (try_wait_asleep(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!try_wait_asleep(bar, parity)) {
+        if (*abort_flag) return false;
+        if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
+            *abort_flag = 1;
+            atomicCAS(status, 0, (int)PM_ERR_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
 __device__ __forceinline__ float ex2f(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// V block as the MN-major B operand of O += P V: 64-wide pieces of the head dim lie 16 KB apart
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 2^x of a pair without the special-function unit: x = n + f with n whole and |f| <= 1/2 by adding a large number, 2^f by a cubic (least
+// largest relative error, 2^-13.7; the rounding of P to bf16 is up to 2^-8), 2^n from the exponent bits.  x <= 127; below -126 the result is
+// 2^-126.  A NaN stays one.
+__device__ __forceinline__ uint64_t ex2_poly(uint64_t z) {
+    constexpr float BIG = 12582912.f + 127.f;                 // 1.5 * 2^23; the last bits of t hold n + 127
+    float x0, x1, t0, t1;
+    upk2(z, x0, x1);
+    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x0) : "f"(x0));             // -126
+    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x1) : "f"(x1));
+    const uint64_t x = pk2(x0, x1), t = add2(x, pk2(BIG, BIG)), f = fma2(add2(t, pk2(-BIG, -BIG)), pk2(-1.f, -1.f), x);
+    uint64_t p = fma2(f, pk2(0.055171322f, 0.055171322f), pk2(0.24261133f, 0.24261133f));
+    p = fma2(p, f, pk2(0.69326109f, 0.69326109f));
+    p = fma2(p, f, pk2(0.99992806f, 0.99992806f));
+    upk2(t, t0, t1);
+    return mul2(p, pk2(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23)));
+}
+// hidden keys, and columns that were not formed, count as -inf
+template <int N>
+__device__ __forceinline__ void hide(uint32_t* v, int lim) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = e < lim ? v[e] : 0xFF800000u;
+}
+template <int N>
+__device__ __forceinline__ float max_of(const uint32_t* v, float m) {
+    float t[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int e = 0; e < N; e += 2) t[(e >> 1) & 3] = max3(t[(e >> 1) & 3], __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+    return fmaxf(max3(t[0], t[1], t[2]), t[3]);
+}
+// V block as the MN-major B operand of O += P V: 64-wide pieces of the head dim lie one behind the other
 template <int D>
 __device__ __forceinline__ uint64_t v_desc(uint32_t saddr) {
     return D == 64 ? smem_desc(saddr, 128)
-                   : ((uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)(16384 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61));
+                   : ((uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)(PT_KEYS * 128 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61));
 }
 __device__ __forceinline__ int round16(int n) { return (n + 15) & ~15; }
 // Whether the unit's last value block holds rows behind the sequence's last key that a product reads (it takes keys by 16).  That block
-// lands on a barrier of its own, where warp 14 awaits it, and warp 14 passes it on to those who await the ring.
+// lands on a barrier of its own, where warp 10 awaits it, and passes it on to those who await the ring.
 __device__ __forceinline__ bool has_tail(const PtUnit& u) {
     const int blocks = max(u.blocks0, u.blocks1);
     return blocks * PT_KEYS > u.nk && (u.nk & 15) != 0;
@@ -120,9 +176,9 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
         if (threadIdx.x == 0) atomicCAS(a.status, 0, (int)PM_ERR_CUDA);
         return;
     }
-    PtControl<D>& ctl = *reinterpret_cast<PtControl<D>*>(smem_raw + (Lay::Q_SLOTS + Lay::KV_SLOTS) * Lay::SLOT);
-    auto q_s = [&](int slot) { return base + (uint32_t)(slot * Lay::SLOT); };
-    auto kv_s = [&](int slot) { return base + (uint32_t)((Lay::Q_SLOTS + slot) * Lay::SLOT); };
+    PtControl<D>& ctl = *reinterpret_cast<PtControl<D>*>(smem_raw + Lay::Q_SLOTS * Lay::Q_BYTES + Lay::KV_SLOTS * Lay::KV_BYTES);
+    auto q_s = [&](int slot) { return base + (uint32_t)(slot * Lay::Q_BYTES); };
+    auto kv_s = [&](int slot) { return base + (uint32_t)(Lay::Q_SLOTS * Lay::Q_BYTES + slot * Lay::KV_BYTES); };
     auto bar = [&](const unsigned long long& b) { return smem_u32(&b); };
     volatile int* abort_flag = &ctl.abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -130,21 +186,21 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < Lay::Q_SLOTS; ++i) { mbar_init(bar(ctl.q_full[i]), 1); mbar_init(bar(ctl.q_empty[i]), 1); }
-        for (int i = 0; i < Lay::KV_SLOTS; ++i) { mbar_init(bar(ctl.kv_full[i]), 1); mbar_init(bar(ctl.kv_empty[i]), 1); }
+        for (int i = 0; i < Lay::KV_SLOTS; ++i) { mbar_init(bar(ctl.kv_full[i]), 1); mbar_init(bar(ctl.kv_empty[i]), 2); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(ctl.s_ready[i]), 1); mbar_init(bar(ctl.s_read[i]), 4); mbar_init(bar(ctl.p_ready[i]), 4); mbar_init(bar(ctl.pv_done[i]), 1);
-            mbar_init(bar(ctl.o_ready[i]), 1); mbar_init(bar(ctl.o_read[i]), 4); mbar_init(bar(ctl.l_ready[i]), 4);
+            for (int b = 0; b < 2; ++b) { mbar_init(bar(ctl.s_ready[i][b]), 1); mbar_init(bar(ctl.p_ready[i][b]), PT_SOFTMAX); }
+            mbar_init(bar(ctl.pv_done[i]), 1); mbar_init(bar(ctl.o_ready[i]), 1);
         }
         for (int i = 0; i < PT_TAILS; ++i) mbar_init(bar(ctl.tail[i]), 1);
-        // consumers of a unit: twelve softmax and output warps, the issuing thread, warp 14
-        for (int i = 0; i < PT_UNITS; ++i) { mbar_init(bar(ctl.unit_full[i]), 1); mbar_init(bar(ctl.unit_empty[i]), 14); }
+        // consumers of a unit: the softmax warps, the two issuing threads, warp 10
+        for (int i = 0; i < PT_UNITS; ++i) { mbar_init(bar(ctl.unit_full[i]), 1); mbar_init(bar(ctl.unit_empty[i]), 2 * PT_SOFTMAX + 3); }
         ctl.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncwarp();
-    if (warp == 12) {
-        tmem_alloc(smem_u32(&ctl.tmem), 512);
+    if (warp == 8) {
+        tmem_alloc(smem_u32(&ctl.tmem), Lay::TMEM);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -155,200 +211,178 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
 
     // unit number n of this CTA; false once the CTA is aborting
     auto take_unit = [&](uint32_t n, PtUnit& u) {
-        if (!mbar_wait(bar(ctl.unit_full[n % PT_UNITS]), (n / PT_UNITS) & 1u, abort_flag, a.status)) return false;
+        if (!wait_asleep(bar(ctl.unit_full[n % PT_UNITS]), (n / PT_UNITS) & 1u, abort_flag, a.status)) return false;
         const int4* p = reinterpret_cast<const int4*>(&ctl.units[n % PT_UNITS]);
         const int4 x = p[0], y = p[1];
         u = PtUnit{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
         return true;
     };
 
-    if (warp < 8) {
-        // ------------------------------------------------------------------ softmax
-        regs_up<PT_REGS_SOFTMAX>();
-        const int tile = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + lanes + Lay::s_col(tile), t_p = tmem + lanes + Lay::p_col(tile), t_o = tmem + lanes + Lay::o_col(tile);
-        const int row_tok = row / a.group;
+    if (warp < 2 * PT_SOFTMAX) {
+        // ------------------------------------------------------------------ softmax, output
+        const int tile = warp / PT_SOFTMAX, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_o = lanes + Lay::o_col(tile);
         const float c = a.c, lag = PT_LAG / a.c;
         const uint64_t c2 = pk2(c, c);
-        uint32_t steps = 0, sums = 0;                         // blocks, tiles so far
+        uint32_t steps = 0, tiles = 0;                        // blocks, tiles with blocks so far
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
-            PtUnit u;
-            ok = take_unit(n, u);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
-            if (lane == 0) mbar_arrive(bar(ctl.unit_empty[n % PT_UNITS]));
-            if (u.blocks0 < 0) break;
-            const int blocks = tile ? u.blocks1 : u.blocks0;
-            if (blocks == 0) continue;
-            const Segment seg{u.q0, u.nq, u.k0, u.nk};
-            const int tok0 = u.tok0 + tile * TT;
-            const int vis = packed_visible(seg, min(tok0 + row_tok, u.nq - 1), a.causal);
-            const int vis_all = packed_visible(seg, tok0, a.causal);         // keys that every row sees
-            const int vis_end = packed_visible(seg, min(tok0 + TT, u.nq) - 1, a.causal);
-            float m = -INFINITY, l = 0.f;
+            int blocks, vis, vis_all, vis_end;                // vis_all: keys that every row sees
+            {
+                PtUnit u;
+                ok = take_unit(n, u);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                blocks = tile ? u.blocks1 : u.blocks0;
+                const Segment seg{u.q0, u.nq, u.k0, u.nk};
+                const int tok0 = u.tok0 + tile * TT;
+                vis = packed_visible(seg, min(tok0 + row / a.group, u.nq - 1), a.causal);
+                vis_all = packed_visible(seg, tok0, a.causal);
+                vis_end = packed_visible(seg, min(tok0 + TT, u.nq) - 1, a.causal);
+                if (u.blocks0 < 0) break;
+            }
+            float m = -INFINITY;
+            uint64_t sum0 = pk2(0.f, 0.f), sum1 = sum0;
             for (int j = 0; j < blocks; ++j, ++steps) {
+                const uint32_t buffer = steps % 2, t_s = lanes + Lay::s_col(tile, buffer);
                 const int ncols = round16(min(PT_KEYS, vis_end - j * PT_KEYS));
-                ok = mbar_wait(bar(ctl.s_ready[tile]), steps & 1u, abort_flag, a.status);
+                // a block whose keys all rows see takes a path without conditions
+                const bool whole = vis_all >= (j + 1) * PT_KEYS;
+                ok = wait_asleep(bar(ctl.s_ready[tile][buffer]), (steps / 2) & 1u, abort_flag, a.status);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t v[128];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (k * 32 < ncols) tmem_ld32(t_s + k * 32, v + k * 32);
-                tmem_ld_wait();
-                if (Lay::OWN_P) {                             // the scores are in registers: the next ones may take their place
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(ctl.s_read[tile]));
+                uint32_t v[PT_KEYS];
+                float top;
+                if (whole) {
+                    tmem_ld32(t_s, v);
+                    tmem_ld32(t_s + 32, v + 32);
+                    tmem_ld_wait();
+                    top = max_of<64>(v, -INFINITY);
+                } else {                                      // by 16 columns, twice
+                    top = -INFINITY;
+#pragma unroll 1
+                    for (int k = 0; k < ncols; k += 16) {
+                        tmem_ld16(t_s + k, v);
+                        tmem_ld_wait();
+                        hide<16>(v, vis - j * PT_KEYS - k);
+                        top = max_of<16>(v, top);
+                    }
                 }
-                const int lim = vis - j * PT_KEYS;
-                if (vis_all < (j + 1) * PT_KEYS) {            // hidden keys, and columns that were not formed
-#pragma unroll
-                    for (int e = 0; e < 128; ++e) v[e] = e < lim ? v[e] : 0xFF800000u;
-                }
-                float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (k * 32 < ncols)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) t[e & 3] = fmaxf(t[e & 3], __uint_as_float(v[k * 32 + e]));
-                const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
                 if (j == 0) {
                     m = top;
                 } else if (__any_sync(0xFFFFFFFFu, top > m + lag)) {
                     // what is there comes down to the new maximum, once the product before has been added
                     const float up = fmaxf(m, top), f = up == m ? 1.f : ex2f((m - up) * c);
                     m = up;
-                    l *= f;
-                    ok = mbar_wait(bar(ctl.pv_done[tile]), (steps - 1) & 1u, abort_flag, a.status);
+                    sum0 = mul2(sum0, pk2(f, f));
+                    sum1 = mul2(sum1, pk2(f, f));
+                    ok = wait_asleep(bar(ctl.pv_done[tile]), (steps - 1) & 1u, abort_flag, a.status);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) break;
                     tc_fence_after();
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        uint32_t o[16];
-                        tmem_ld16(t_o + k * 16, o);
+#pragma unroll 1
+                    for (int k = 0; k < D; k += 8) {
+                        uint32_t o[8];
+                        tmem_ld8(t_o + k, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st16(t_o + k * 16, o);
+                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st8(t_o + k, o);
                     }
-                }
-                if (Lay::OWN_P && steps > 0) {                // the product before has read its probabilities
-                    ok = mbar_wait(bar(ctl.pv_done[tile]), (steps - 1) & 1u, abort_flag, a.status);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) break;
-                    tc_fence_after();
                 }
                 const float mc = m == -INFINITY ? 0.f : -m * c;              // a row that sees nothing: all terms 0
                 const uint64_t mc2 = pk2(mc, mc);
-                uint64_t sum0 = pk2(0.f, 0.f), sum1 = sum0;
+                // 16 scores, P to `to`; POLY: of the eight pairs that many by ex2_poly
+                auto terms = [&](const uint32_t* x16, uint32_t to, auto poly) {
+                    uint32_t pk[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (k * 32 < ncols) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float x, y;
-                            upk2(fma2(pk2(__uint_as_float(v[k * 32 + e]), __uint_as_float(v[k * 32 + e + 1])), c2, mc2), x, y);
+                    for (int e = 0; e < 8; ++e) {
+                        uint64_t p = fma2(pk2(__uint_as_float(x16[2 * e]), __uint_as_float(x16[2 * e + 1])), c2, mc2);
+                        float x, y;
+                        if (e >= 8 - decltype(poly)::value) {
+                            p = ex2_poly(p);
+                            upk2(p, x, y);
+                        } else {
+                            upk2(p, x, y);
                             x = ex2f(x);
                             y = ex2f(y);
-                            if (e & 2) sum1 = add2(sum1, pk2(x, y));
-                            else sum0 = add2(sum0, pk2(x, y));
-                            pk[e >> 1] = pack_bf16(x, y);
+                            p = pk2(x, y);
                         }
-                        tmem_st16(t_p + k * 16, pk);
+                        if (e & 1) sum1 = add2(sum1, p);
+                        else sum0 = add2(sum0, p);
+                        pk[e] = pack_bf16(x, y);
                     }
-                float s0, s1;
-                upk2(add2(sum0, sum1), s0, s1);
-                l += s0 + s1;
+                    tmem_st8(to, pk);
+                };
+                // P of a piece lies over scores that have been read before it is stored
+                if (whole) {
+                    constexpr std::integral_constant<int, PT_POLY> poly;
+#pragma unroll
+                    for (int k = 0; k < PT_KEYS; k += 16) terms(v + k, t_s + k / 2, poly);
+                } else {
+#pragma unroll 1
+                    for (int k = 0; k < ncols; k += 16) {
+                        tmem_ld16(t_s + k, v);
+                        tmem_ld_wait();
+                        hide<16>(v, vis - j * PT_KEYS - k);
+                        terms(v, t_s + k / 2, std::integral_constant<int, 0>());
+                    }
+                }
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(ctl.p_ready[tile]));
+                if (lane == 0) mbar_arrive(bar(ctl.p_ready[tile][buffer]));
             }
             if (!ok) break;
-            // Read by the output warps before o_read is signalled.  A buffer comes up again SUMS tiles later: scores of a tile are formed after
-            // the product of the tile before it (own P: of the one before that) was issued, which waited for o_read of the tile before that.
-            ctl.sums[sums % Lay::SUMS][tile][row] = l;
-            ++sums;
+            float inv = 0.f;
+            if (blocks > 0) {
+                ok = wait_asleep(bar(ctl.o_ready[tile]), tiles & 1u, abort_flag, a.status);
+                ++tiles;
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                float x, y;
+                upk2(add2(sum0, sum1), x, y);
+                inv = x + y == 0.f ? 0.f : 1.f / (x + y);
+            }
+            // read again: the loop above needs the registers
+            const volatile PtUnit& u = ctl.units[n % PT_UNITS];
+            const int row_tok = row / a.group, tok = u.tok0 + tile * TT + row_tok;
+            const bool real = row_tok < TT && tok < u.nq;
+            bf16* to = (bf16*)a.out + (long long)(u.q0 + tok) * a.out_stride + (u.kv_head * a.group + row % a.group) * D;
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(ctl.l_ready[tile]));
-        }
-    } else if (warp < 12) {
-        // ------------------------------------------------------------------ output
-        regs_down<PT_REGS_OUT>();
-        const int row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const int row_tok = row / a.group, head = row % a.group;
-        uint32_t done[2] = {0, 0};
-        bool ok = true;
-        for (uint32_t n = 0; ok; ++n) {
-            PtUnit u;
-            ok = take_unit(n, u);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
             if (lane == 0) mbar_arrive(bar(ctl.unit_empty[n % PT_UNITS]));
-            if (u.blocks0 < 0) break;
 #pragma unroll
-            for (int tile = 0; tile < 2; ++tile) {
-                const int blocks = tile ? u.blocks1 : u.blocks0, tok = u.tok0 + tile * TT + row_tok;
-                const bool real = row_tok < TT && tok < u.nq;
-                bf16* to = (bf16*)a.out + (long long)(u.q0 + tok) * a.out_stride + (u.kv_head * a.group + head) * D;
-                float inv = 0.f;
+            for (int k = 0; k < D; k += 32) {
+                uint32_t o[32];
                 if (blocks > 0) {
-                    ok = mbar_wait(bar(ctl.l_ready[tile]), done[tile] & 1u, abort_flag, a.status);
-                    ok = ok && mbar_wait(bar(ctl.o_ready[tile]), done[tile] & 1u, abort_flag, a.status);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const float l = ctl.sums[done[tile] % Lay::SUMS][tile][row];
-                    inv = l == 0.f ? 0.f : 1.f / l;
-                    ++done[tile];
+                    tmem_ld32(t_o + k, o);
+                    tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0u;
                 }
-                const uint32_t t_o = tmem + lanes + Lay::o_col(tile);
 #pragma unroll
-                for (int k = 0; k < D / 32; ++k) {
-                    uint32_t o[32];
-                    if (blocks > 0) {
-                        tmem_ld32(t_o + k * 32, o);
-                        tmem_ld_wait();
-                    } else {
+                for (int e = 0; e < 16; ++e) o[e] = pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+                if (real)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0u;
-                    }
-                    if (real)
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t w[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                w[e] = pack_bf16(__uint_as_float(o[q * 16 + 2 * e]) * inv, __uint_as_float(o[q * 16 + 2 * e + 1]) * inv);
-                            *reinterpret_cast<uint4*>(to + k * 32 + q * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-                            *reinterpret_cast<uint4*>(to + k * 32 + q * 16 + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-                        }
-                }
-                if (blocks > 0) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(ctl.o_read[tile]));
-                }
+                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + k + 2 * e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
             }
+            // O is in registers before the next unit's first P is announced, and that comes before the product that overwrites it
+            tc_fence_before();
         }
     } else {
-        regs_down<PT_REGS_ISSUE>();
-        if (warp == 12) {
+        if (warp == 8 || warp == 11) {
             if (elect_one()) {
-                // -------------------------------------------------------------- MMA issue
-                // Steps: key block j of a unit, for the tiles that have it.  kv: ring position of the step's K block (V follows it).
-                struct Step { PtUnit u; int j, blocks; uint32_t kv, q[2]; };
-                const uint32_t idesc_pv = instr_desc_b_mn(D);
-                uint32_t units = 0, kv_next = 0, q_next = 0;
-                uint32_t s_count[2] = {0, 0}, p_count[2] = {0, 0}, o_count[2] = {0, 0};
-                bool ok = true, more = true;
+                // -------------------------------------------------------------- MMA issue, a thread for each tile
+                // Steps: key blocks of the units, in order; kv: ring position of a step's K block (V follows it).  A step that the other tile has
+                // alone only passes the ring on -- not before the block has landed, or the signal would count for the slot's use before.
+                struct Step { PtUnit u; int j, blocks, mine; uint32_t kv, q; };
+                const int i = warp == 8 ? 0 : 1;
+                const uint32_t idesc_pv = instr_desc_b_mn(D), idesc_s = instr_desc(PT_KEYS), t_o = tmem + Lay::o_col(i);
+                uint32_t units = 0, kv_next = 0, q_next = 0, s_count = 0, p_count = 0;
+                bool ok = true;
                 // the step after `s`, or the next unit's first; false: none
                 auto advance = [&](Step& s, bool first) {
                     if (!first && s.j + 1 < s.blocks) {
@@ -369,80 +403,70 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     s.j = 0;
                     s.kv = kv_next;
                     kv_next += 2;
-                    s.q[0] = s.q[1] = 0;
-                    if (s.u.blocks0 > 0) s.q[0] = q_next++;
-                    if (s.u.blocks1 > 0) s.q[1] = q_next++;
+                    s.mine = i ? s.u.blocks1 : s.u.blocks0;
+                    if (s.u.blocks0 > 0) { if (i == 0) s.q = q_next; ++q_next; }
+                    if (s.u.blocks1 > 0) { if (i == 1) s.q = q_next; ++q_next; }
                     return true;
                 };
-                auto has = [&](const Step& s, int i) { return s.j < (i ? s.u.blocks1 : s.u.blocks0); };
-                // the last of a step's tiles to use its K and V blocks
-                auto last_tile = [&](const Step& s) { return has(s, 1) ? 1 : 0; };
-                auto issue_s = [&](const Step& s, int i) {
-                    if (Lay::OWN_P) {                         // the tile's scores before must have been read
-                        ok = mbar_wait(bar(ctl.s_read[i]), (s_count[i] & 1u) ^ 1u, abort_flag, a.status);
-                        if (!ok) return;
+                auto full = [&](uint32_t at) { return wait_asleep(bar(ctl.kv_full[at % Lay::KV_SLOTS]), (at / Lay::KV_SLOTS) & 1u, abort_flag, a.status); };
+                auto scores = [&](const Step& s) {
+                    const uint32_t k_slot = s.kv % Lay::KV_SLOTS;
+                    if (s.j >= s.mine) {
+                        ok = full(s.kv);
+                        mbar_arrive(bar(ctl.kv_empty[k_slot]));
+                        return;
                     }
-                    ++s_count[i];
-                    const int q_slot = (int)(s.q[i] % Lay::Q_SLOTS), k_slot = (int)(s.kv % Lay::KV_SLOTS);
-                    if (s.j == 0) ok = mbar_wait(bar(ctl.q_full[q_slot]), (s.q[i] / Lay::Q_SLOTS) & 1u, abort_flag, a.status);
-                    ok = ok && mbar_wait(bar(ctl.kv_full[k_slot]), (s.kv / Lay::KV_SLOTS) & 1u, abort_flag, a.status);
+                    const uint32_t q_slot = s.q % Lay::Q_SLOTS, buffer = s_count++ & 1u, to = tmem + Lay::s_col(i, buffer);
+                    const uint64_t dq = smem_desc(q_s((int)q_slot), 128), dk = smem_desc(kv_s((int)k_slot), 128);
+                    const uint32_t idesc = s.j + 1 < s.mine ? idesc_s : instr_desc(round16(block_keys(s.u, i, s.j, TT, a.causal)));
+                    if (s.j == 0) ok = wait_asleep(bar(ctl.q_full[q_slot]), (s.q / Lay::Q_SLOTS) & 1u, abort_flag, a.status);
+                    ok = ok && full(s.kv);
                     if (!ok) return;
                     tc_fence_after();
-                    const uint32_t idesc = instr_desc(round16(block_keys(s.u, i, s.j, TT, a.causal)));
-                    const uint64_t dq = smem_desc(q_s(q_slot), 128), dk = smem_desc(kv_s(k_slot), 128);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint64_t at = (uint64_t)((k / 4) * (16384 >> 4) + 2 * (k % 4));
-                        umma_bf16(tmem + Lay::s_col(i), dq + at, dk + at, idesc, k > 0);
-                    }
-                    umma_commit(bar(ctl.s_ready[i]));
-                    if (i == last_tile(s)) umma_commit(bar(ctl.kv_empty[k_slot]));
-                    if (s.j + 1 == (i ? s.u.blocks1 : s.u.blocks0)) umma_commit(bar(ctl.q_empty[q_slot]));
+                    for (int k = 0; k < D / 16; ++k)          // 64-wide pieces of the head dim lie one behind the other
+                        umma_bf16(to, dq + (uint64_t)((k / 4) * (PT_ROWS * 128 >> 4) + 2 * (k % 4)), dk + (uint64_t)((k / 4) * (PT_KEYS * 128 >> 4) + 2 * (k % 4)), idesc, k > 0);
+                    umma_commit(bar(ctl.s_ready[i][buffer]));
+                    umma_commit(bar(ctl.kv_empty[k_slot]));
+                    if (s.j + 1 == s.mine) umma_commit(bar(ctl.q_empty[q_slot]));
                 };
-                auto issue_pv = [&](const Step& s, int i) {
-                    const int blocks = i ? s.u.blocks1 : s.u.blocks0;
-                    const uint32_t at = s.kv + 1;
-                    const int v_slot = (int)(at % Lay::KV_SLOTS);
-                    ok = mbar_wait(bar(ctl.p_ready[i]), p_count[i] & 1u, abort_flag, a.status);
-                    ++p_count[i];
-                    ok = ok && mbar_wait(bar(ctl.kv_full[v_slot]), (at / Lay::KV_SLOTS) & 1u, abort_flag, a.status);
-                    // the tile's output before has been read
-                    if (ok && s.j == 0) {
-                        ok = mbar_wait(bar(ctl.o_read[i]), (o_count[i] & 1u) ^ 1u, abort_flag, a.status);
-                        ++o_count[i];
+                auto product = [&](const Step& s) {
+                    const uint32_t v_slot = (s.kv + 1) % Lay::KV_SLOTS;
+                    ok = full(s.kv + 1);
+                    if (s.j >= s.mine) {
+                        mbar_arrive(bar(ctl.kv_empty[v_slot]));
+                        return;
                     }
+                    const uint32_t buffer = p_count & 1u, p = tmem + Lay::s_col(i, buffer);
+                    const uint64_t dv = v_desc<D>(kv_s((int)v_slot));
+                    const int pieces = s.j + 1 < s.mine ? PT_KEYS / 16 : round16(block_keys(s.u, i, s.j, TT, a.causal)) / 16;
+                    const uint32_t add = s.j > 0 ? 1u : 0u;
+                    ok = ok && wait_asleep(bar(ctl.p_ready[i][buffer]), (p_count++ >> 1) & 1u, abort_flag, a.status);
                     if (!ok) return;
                     tc_fence_after();
-                    const int pieces = round16(block_keys(s.u, i, s.j, TT, a.causal)) / 16;
-                    const uint64_t dv = v_desc<D>(kv_s(v_slot));
-                    for (int k = 0; k < pieces; ++k)
-                        umma_bf16_ts(tmem + Lay::o_col(i), tmem + Lay::p_col(i) + 8 * k, dv + 128 * k, idesc_pv, (s.j > 0 || k > 0) ? 1u : 0u);
+                    if (pieces == PT_KEYS / 16) {
+#pragma unroll
+                        for (int k = 0; k < PT_KEYS / 16; ++k) umma_bf16_ts(t_o, p + 8 * k, dv + 128 * k, idesc_pv, k > 0 ? 1u : add);
+                    } else {
+                        for (int k = 0; k < pieces; ++k) umma_bf16_ts(t_o, p + 8 * k, dv + 128 * k, idesc_pv, k > 0 ? 1u : add);
+                    }
                     umma_commit(bar(ctl.pv_done[i]));
-                    if (i == last_tile(s)) umma_commit(bar(ctl.kv_empty[v_slot]));
-                    if (s.j + 1 == blocks) umma_commit(bar(ctl.o_ready[i]));
+                    umma_commit(bar(ctl.kv_empty[v_slot]));
+                    if (s.j + 1 == s.mine) umma_commit(bar(ctl.o_ready[i]));
                 };
                 Step cur, next;
-                more = advance(cur, true);
-                if (more) {
-                    for (int i = 0; i < 2 && ok; ++i)
-                        if (has(cur, i)) issue_s(cur, i);
-                }
+                bool more = advance(cur, true);
+                if (more) scores(cur);
                 while (more && ok) {
                     next = cur;
                     more = advance(next, false);
                     if (!ok) break;
-                    if (Lay::OWN_P) {
-                        for (int i = 0; i < 2 && ok; ++i)
-                            if (more && has(next, i)) issue_s(next, i);
-                    }
-                    for (int i = 0; i < 2 && ok; ++i) {
-                        if (has(cur, i)) issue_pv(cur, i);
-                        if (!Lay::OWN_P && ok && more && has(next, i)) issue_s(next, i);
-                    }
+                    if (more) scores(next);                   // the other buffer's product has been issued
+                    if (ok) product(cur);
                     cur = next;
                 }
             }
-        } else if (warp == 13) {
+        } else if (warp == 9) {
             // ------------------------------------------------------------------ units and loads
             dep_wait();                                       // everything else follows from what is read here
             const int n_seqs = a.n_seqs, per_unit = 2 * TT;
@@ -483,7 +507,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     left += gridDim.x;
                 }
                 const int at = (int)(units % PT_UNITS);
-                ok = mbar_wait(bar(ctl.unit_empty[at]), ((units / PT_UNITS) & 1u) ^ 1u, abort_flag, a.status);
+                ok = wait_asleep(bar(ctl.unit_empty[at]), ((units / PT_UNITS) & 1u) ^ 1u, abort_flag, a.status);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 if (lane == 0) {
@@ -500,20 +524,20 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 if (elect_one()) {
                     auto load_q = [&](int i) {
                         const int slot = (int)(q % Lay::Q_SLOTS);
-                        ok = ok && mbar_wait(bar(ctl.q_empty[slot]), ((q / Lay::Q_SLOTS) & 1u) ^ 1u, abort_flag, a.status);
+                        ok = ok && wait_asleep(bar(ctl.q_empty[slot]), ((q / Lay::Q_SLOTS) & 1u) ^ 1u, abort_flag, a.status);
                         if (!ok) return;
                         mbar_expect_tx(bar(ctl.q_full[slot]), (uint32_t)(TT * a.group * D * 2));
                         for (int x = 0; x < D / 64; ++x)
-                            tma_load_3d(q_s(slot) + x * 16384, &tm_q, x * 64, u.kv_head * a.group, u.q0 + u.tok0 + i * TT, bar(ctl.q_full[slot]));
+                            tma_load_3d(q_s(slot) + x * PT_ROWS * 128, &tm_q, x * 64, u.kv_head * a.group, u.q0 + u.tok0 + i * TT, bar(ctl.q_full[slot]));
                         ++q;
                     };
                     auto load_kv = [&](const CUtensorMap* tm, int j, unsigned long long* full) {
                         const int slot = (int)(kv % Lay::KV_SLOTS);
-                        ok = ok && mbar_wait(bar(ctl.kv_empty[slot]), ((kv / Lay::KV_SLOTS) & 1u) ^ 1u, abort_flag, a.status);
+                        ok = ok && wait_asleep(bar(ctl.kv_empty[slot]), ((kv / Lay::KV_SLOTS) & 1u) ^ 1u, abort_flag, a.status);
                         if (!ok) return;
                         const uint32_t on = full ? bar(*full) : bar(ctl.kv_full[slot]);
-                        mbar_expect_tx(on, (uint32_t)Lay::SLOT);
-                        for (int x = 0; x < D / 64; ++x) tma_load_3d(kv_s(slot) + x * 16384, tm, x * 64, u.kv_head, u.k0 + j * PT_KEYS, on);
+                        mbar_expect_tx(on, (uint32_t)Lay::KV_BYTES);
+                        for (int x = 0; x < D / 64; ++x) tma_load_3d(kv_s(slot) + x * PT_KEYS * 128, tm, x * 64, u.kv_head, u.k0 + j * PT_KEYS, on);
                         ++kv;
                     };
                     for (int j = 0; j < blocks && ok; ++j) {
@@ -529,7 +553,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 kv = __reduce_max_sync(0xFFFFFFFFu, kv);
                 q = __reduce_max_sync(0xFFFFFFFFu, q);
             }
-        } else if (warp == 14) {
+        } else if (warp == 10) {
             // ------------------------------------------------------------------ values behind a sequence's last key
             uint32_t kv = 0, tails = 0;
             bool ok = true;
@@ -544,14 +568,14 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 kv += 2 * (uint32_t)blocks;
                 if (!has_tail(u)) continue;
                 const int slot = (int)((kv - 1) % Lay::KV_SLOTS);
-                ok = mbar_wait(bar(ctl.tail[tails % PT_TAILS]), (tails / PT_TAILS) & 1u, abort_flag, a.status);
+                ok = wait_asleep(bar(ctl.tail[tails % PT_TAILS]), (tails / PT_TAILS) & 1u, abort_flag, a.status);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 ++tails;
                 const int first = u.nk - (blocks - 1) * PT_KEYS, rows = round16(first) - first;
                 for (int i = lane; i < rows * D / 8; i += 32) {              // whole rows, so their swizzle does not matter
                     const int r = first + i / (D / 8), c = i % (D / 8);
-                    st_shared_v4(kv_s(slot) + (uint32_t)((c / 8) * 16384 + r * 128 + (c % 8) * 16), make_uint4(0, 0, 0, 0));
+                    st_shared_v4(kv_s(slot) + (uint32_t)((c / 8) * PT_KEYS * 128 + r * 128 + (c % 8) * 16), make_uint4(0, 0, 0, 0));
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -568,9 +592,9 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 8) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, Lay::TMEM);
     }
 }
 
