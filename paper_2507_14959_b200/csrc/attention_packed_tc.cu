@@ -18,7 +18,8 @@
 // special-function unit, the next limit, sees a third.  So several tiles take turns on an SM: with head dim 64 two CTAs of two tiles each
 // (half of tensor memory: 64 columns of S and 64 of O a tile), with 128 one CTA whose tiles have two buffers of S, so that
 // the next scores are formed meanwhile.
-// Units are visited from the last rows of the sequences to the first, so in causal order the long ones come first.
+// Units are visited by falling cost, there and back over the CTAs: up to PT_SORTED sequences are ranked by every CTA when it starts (more of
+// them are taken in their own order).
 #include <algorithm>
 #include <type_traits>
 
@@ -33,16 +34,17 @@ constexpr int PT_SOFTMAX = 4;                                 // softmax warps o
 constexpr int PT_THREADS = 32 * (2 * PT_SOFTMAX + 4);
 constexpr int PT_ROWS = 128;                                  // rows of a tile
 constexpr int PT_KEYS = 64;                                   // keys of a block
+constexpr int PT_SORTED = 256;                                // sequences up to which a CTA ranks them
 constexpr int PT_UNITS = 4;                                   // units announced ahead
 constexpr int PT_TAILS = 2 * PT_UNITS;                        // barriers of value blocks to be cleared; the loads are at most PT_UNITS units ahead of warp 10
-constexpr int PT_POLY = 2;                                    // of eight pairs of exponentials, those worked out by ex2_poly
+constexpr int PT_POLY = 1;                                    // of eight pairs of exponentials, those worked out by ex2_poly
 constexpr float PT_LAG = 8.f;                                 // log2 of how far a row's terms may exceed 1
 
 template <int D>
 struct PtLayout {
     static constexpr uint32_t TMEM = 512;
     static constexpr int Q_BYTES = PT_ROWS * D * 2, KV_BYTES = PT_KEYS * D * 2;       // of a tile's queries, of a K or V block
-    static constexpr int Q_SLOTS = D == 64 ? 4 : 3, KV_SLOTS = D == 64 ? 12 : 8;
+    static constexpr int Q_SLOTS = D == 64 ? 4 : 3, KV_SLOTS = D == 64 ? 12 : 7;
     // a tile's columns: two buffers of scores, O
     static __host__ __device__ constexpr uint32_t s_col(int i, uint32_t buffer) { return i * 256 + buffer * PT_KEYS; }
     static __host__ __device__ constexpr uint32_t o_col(int i) { return i * 256 + 2 * PT_KEYS; }
@@ -55,6 +57,9 @@ struct PtUnit {                                               // 32 bytes
 
 template <int D>
 struct PtControl {
+    Segment sorted[PT_SORTED];                                // by falling cost
+    int before[PT_SORTED];                                    // units of the sequences ahead of it
+    int key[PT_SORTED], count[PT_SORTED];                     // in the caller's order: cost, units
     PtUnit units[PT_UNITS];
     unsigned long long q_full[PtLayout<D>::Q_SLOTS], q_empty[PtLayout<D>::Q_SLOTS];
     unsigned long long kv_full[PtLayout<D>::KV_SLOTS], kv_empty[PtLayout<D>::KV_SLOTS];
@@ -75,7 +80,18 @@ struct PtArgs {
     int tile_tokens;                                          // TT
 };
 
-// Bounded wait in which the hardware lets the warp sleep.
+// Bounded wait in which the hardware lets the warp sleep, after a look that costs less than falling asleep.
+__device__ __forceinline__ uint32_t test_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok;
+}
 __device__ __forceinline__ uint32_t try_wait_asleep(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
@@ -88,7 +104,7 @@ __device__ __forceinline__ uint32_t try_wait_asleep(uint32_t bar, uint32_t parit
     return ok;
 }
 __device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
-    if (try_wait_asleep(bar, parity)) return true;
+    if (test_wait(bar, parity)) return true;
     const long long t0 = clock64();
     while (!try_wait_asleep(bar, parity)) {
         if (*abort_flag) return false;
@@ -203,11 +219,36 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
         tmem_alloc(smem_u32(&ctl.tmem), Lay::TMEM);
         tmem_relinquish();
     }
+    dep_release();
+    dep_wait();                                               // everything below follows from what is read from here on
+    const bool ranked = a.n_seqs <= PT_SORTED;
+    const int per_unit = 2 * TT;
+    if (ranked) {
+        Segment g{0, 0, 0, 0};
+        int key = 0, count = 0;
+        const int me = (int)threadIdx.x;
+        if (me < a.n_seqs) {
+            g = packed_segment(a, me);
+            count = (g.nq + per_unit - 1) / per_unit;
+            key = a.causal ? count : g.nk;
+            ctl.key[me] = key;
+            ctl.count[me] = count;
+        }
+        __syncthreads();
+        if (me < a.n_seqs) {
+            int rank = 0, before = 0;
+            for (int k = 0; k < a.n_seqs; ++k) {
+                const int other = ctl.key[k];
+                if (other > key || (other == key && k < me)) { ++rank; before += ctl.count[k]; }
+            }
+            ctl.sorted[rank] = g;
+            ctl.before[rank] = before;
+        }
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem;
-    dep_release();
 
     // unit number n of this CTA; false once the CTA is aborting
     auto take_unit = [&](uint32_t n, PtUnit& u) {
@@ -293,9 +334,8 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 }
                 const float mc = m == -INFINITY ? 0.f : -m * c;              // a row that sees nothing: all terms 0
                 const uint64_t mc2 = pk2(mc, mc);
-                // 16 scores, P to `to`; POLY: of the eight pairs that many by ex2_poly
-                auto terms = [&](const uint32_t* x16, uint32_t to, auto poly) {
-                    uint32_t pk[8];
+                // 16 scores to eight pairs of terms; POLY: of the eight pairs that many by ex2_poly
+                auto terms = [&](const uint32_t* x16, uint32_t* pk, auto poly) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         uint64_t p = fma2(pk2(__uint_as_float(x16[2 * e]), __uint_as_float(x16[2 * e + 1])), c2, mc2);
@@ -313,20 +353,26 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                         else sum0 = add2(sum0, p);
                         pk[e] = pack_bf16(x, y);
                     }
-                    tmem_st8(to, pk);
                 };
                 // P of a piece lies over scores that have been read before it is stored
                 if (whole) {
                     constexpr std::integral_constant<int, PT_POLY> poly;
 #pragma unroll
-                    for (int k = 0; k < PT_KEYS; k += 16) terms(v + k, t_s + k / 2, poly);
+                    for (int k = 0; k < PT_KEYS; k += 32) {
+                        uint32_t pk[16];
+                        terms(v + k, pk, poly);
+                        terms(v + k + 16, pk + 8, poly);
+                        tmem_st16(t_s + k / 2, pk);
+                    }
                 } else {
 #pragma unroll 1
                     for (int k = 0; k < ncols; k += 16) {
                         tmem_ld16(t_s + k, v);
                         tmem_ld_wait();
                         hide<16>(v, vis - j * PT_KEYS - k);
-                        terms(v, t_s + k / 2, std::integral_constant<int, 0>());
+                        uint32_t pk[8];
+                        terms(v, pk, std::integral_constant<int, 0>());
+                        tmem_st8(t_s + k / 2, pk);
                     }
                 }
                 tmem_st_wait();
@@ -468,43 +514,68 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             }
         } else if (warp == 9) {
             // ------------------------------------------------------------------ units and loads
-            dep_wait();                                       // everything else follows from what is read here
-            const int n_seqs = a.n_seqs, per_unit = 2 * TT;
-            auto units_of = [&](int s) {
-                if (s >= n_seqs) return 0;
-                return (packed_segment(a, s).nq + per_unit - 1) / per_unit;
-            };
-            int most = 0;
-            for (int s = lane; s < n_seqs; s += 32) most = max(most, units_of(s));
-            most = __reduce_max_sync(0xFFFFFFFFu, most);
-            // Walk: level by level from `most` - 1 down, in a level the sequences that reach it, in a sequence the K/V heads.  `left` counts from
-            // the start of the current 32 sequences at the current level.
-            int level = most - 1, block = 0, mine = units_of(lane);
+            // The walk over the units: in causal order level by level, level L holding unit L of each sequence that has one (the sequences with most
+            // units come first, so those are the first `reach`); without it sequence by sequence.  `left` counts K/V heads of units from where the
+            // walk stands; the CTAs take them in turn, there and back, so that none has the longest of every turn.
+            const int n_seqs = a.n_seqs;
+            auto units_of = [&](const Segment& g) { return (g.nq + per_unit - 1) / per_unit; };
+            int level = 0, reach = 0, block = 0;
+            Segment mine{0, 0, 0, 0};                         // not ranked: a sequence per lane
+            if (!ranked) mine = lane < n_seqs ? packed_segment(a, lane) : mine;
+            else if (a.causal) level = units_of(ctl.sorted[0]) - 1;
             long long left = blockIdx.x;
             uint32_t units = 0, kv = 0, q = 0, tails = 0;
             bool ok = true;
             while (ok) {
-                uint32_t set = 0;
-                while (level >= 0) {
-                    set = __ballot_sync(0xFFFFFFFFu, mine > level);
-                    const long long here = (long long)__popc(set) * a.kv_heads;
-                    if (left < here) break;
-                    left -= here;
-                    block += 32;
-                    if (block >= n_seqs) { block = 0; --level; }
-                    if (n_seqs > 32) mine = units_of(block + lane);
+                Segment g{0, 0, 0, 0};
+                int tile = -1;                                // of the sequence, in units
+                if (ranked && a.causal) {
+                    for (; level >= 0; --level) {
+                        while (reach < n_seqs && units_of(ctl.sorted[reach]) > level) ++reach;
+                        const long long here = (long long)reach * a.kv_heads;
+                        if (left < here) {
+                            g = ctl.sorted[left / a.kv_heads];
+                            tile = level;
+                            break;
+                        }
+                        left -= here;
+                    }
+                } else if (ranked) {
+                    const long long at = left / a.kv_heads;   // of all units
+                    while (reach + 1 < n_seqs && ctl.before[reach + 1] <= at) ++reach;
+                    g = ctl.sorted[reach];
+                    if (at - ctl.before[reach] < units_of(g)) tile = (int)(at - ctl.before[reach]);
+                } else {
+                    while (block < n_seqs) {
+                        const int mass = units_of(mine);
+                        int sum = mass;                       // of the lanes up to this one
+#pragma unroll
+                        for (int x = 1; x < 32; x <<= 1) {
+                            const int y = __shfl_up_sync(0xFFFFFFFFu, sum, x);
+                            if (lane >= x) sum += y;
+                        }
+                        const long long here = (long long)__shfl_sync(0xFFFFFFFFu, sum, 31) * a.kv_heads;
+                        if (left < here) {
+                            const int nth = (int)(left / a.kv_heads);
+                            const int from = __ffs((int)__ballot_sync(0xFFFFFFFFu, sum > nth)) - 1;
+                            g = Segment{__shfl_sync(0xFFFFFFFFu, mine.q0, from), __shfl_sync(0xFFFFFFFFu, mine.nq, from), __shfl_sync(0xFFFFFFFFu, mine.k0, from),
+                                        __shfl_sync(0xFFFFFFFFu, mine.nk, from)};
+                            tile = nth - __shfl_sync(0xFFFFFFFFu, sum - mass, from);
+                            break;
+                        }
+                        left -= here;
+                        block += 32;
+                        mine = block + lane < n_seqs ? packed_segment(a, block + lane) : Segment{0, 0, 0, 0};
+                    }
                 }
                 PtUnit u = {0, 0, 0, 0, 0, 0, -1, -1};
-                if (level >= 0) {
-                    int nth = (int)(left / a.kv_heads);
-                    for (; nth > 0; --nth) set &= set - 1;
-                    const Segment g = packed_segment(a, block + __ffs((int)set) - 1);
+                if (tile >= 0) {
                     u.q0 = g.q0; u.nq = g.nq; u.k0 = g.k0; u.nk = g.nk;
-                    u.tok0 = level * per_unit;
+                    u.tok0 = tile * per_unit;
                     u.kv_head = (int)(left % a.kv_heads);
                     u.blocks0 = tile_blocks(g, u.tok0, TT, a.causal);
                     u.blocks1 = tile_blocks(g, u.tok0 + TT, TT, a.causal);
-                    left += gridDim.x;
+                    left += 2 * ((units & 1u) ? (long long)blockIdx.x : (long long)gridDim.x - 1 - blockIdx.x) + 1;
                 }
                 const int at = (int)(units % PT_UNITS);
                 ok = wait_asleep(bar(ctl.unit_empty[at]), ((units / PT_UNITS) & 1u) ^ 1u, abort_flag, a.status);

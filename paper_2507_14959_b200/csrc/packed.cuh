@@ -26,26 +26,21 @@ struct Segment { int q0, nq, k0, nk; };
 // Rows of sequence s.  Lists that are malformed, lie outside the buffers or exceed the call's limits give a sequence without
 // queries, so nothing is read or written because of them.
 __device__ __forceinline__ Segment packed_segment(const PackedArgs& a, int s) {
+    // all loads first: they take as long as one
     const int q0 = a.q_offsets[s], q1 = a.q_offsets[s + 1];
-    int k0 = q0, nk = q1 - q0;
-    bool ok = q0 >= 0 && q1 >= q0 && q1 <= a.q_rows && q1 - q0 <= a.max_q;
-    if (a.kv_offsets) k0 = a.kv_offsets[s];
-    if (a.kv_lengths) nk = a.kv_lengths[s];
-    else if (a.kv_offsets) {
-        const int k1 = a.kv_offsets[s + 1];
-        ok = ok && k0 >= 0 && k1 >= k0;
-        nk = ok ? k1 - k0 : 0;
-    }
-    ok = ok && k0 >= 0 && nk >= 0 && nk <= a.max_kv && (long long)k0 + nk <= a.kv_rows;
+    const int k_at = a.kv_offsets ? a.kv_offsets[s] : q0;
+    const int length = a.kv_lengths ? a.kv_lengths[s] : 0, k_next = a.kv_lengths ? 0 : a.kv_offsets ? a.kv_offsets[s + 1] : q1;
+    const long long n_q = (long long)q1 - q0, n_k = a.kv_lengths ? (long long)length : (long long)k_next - k_at;
+    const bool ok = q0 >= 0 && n_q >= 0 && q1 <= a.q_rows && n_q <= a.max_q && k_at >= 0 && n_k >= 0 && n_k <= a.max_kv && k_at + n_k <= a.kv_rows;
     if (!ok) {
         atomicCAS(a.status, 0, (int)PM_ERR_ARG);
         return Segment{0, 0, 0, 0};
     }
-    return Segment{q0, q1 - q0, k0, nk};
+    return Segment{q0, (int)n_q, k_at, (int)n_k};
 }
-// Keys that query j of a sequence sees.
+// Keys that query j < nq of a sequence sees.
 __device__ __forceinline__ int packed_visible(const Segment& g, int j, int causal) {
-    return causal ? min(g.nk, max(0, j + 1 + g.nk - g.nq)) : g.nk;
+    return causal ? max(0, g.nk - (g.nq - 1 - j)) : g.nk;
 }
 
 }  // namespace
