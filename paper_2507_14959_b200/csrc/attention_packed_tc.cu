@@ -263,23 +263,31 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
         // ------------------------------------------------------------------ softmax, output
         const int tile = warp / PT_SOFTMAX, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_o = lanes + Lay::o_col(tile);
+        const int row_tok = row / a.group, head_at = row % a.group * D;
+        // 32-byte stores, a whole sector each, where the rows allow it
+        const bool sectors = ((uintptr_t)a.out & 31) == 0 && a.out_stride % 16 == 0;
         const float c = a.c, lag = PT_LAG / a.c;
         const uint64_t c2 = pk2(c, c);
         uint32_t steps = 0, tiles = 0;                        // blocks, tiles with blocks so far
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             int blocks, vis, vis_all, vis_end;                // vis_all: keys that every row sees
+            bool real;
+            bf16* to;                                         // this thread's row of the output
             {
                 PtUnit u;
                 ok = take_unit(n, u);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
+                if (lane == 0) mbar_arrive(bar(ctl.unit_empty[n % PT_UNITS]));
                 blocks = tile ? u.blocks1 : u.blocks0;
                 const Segment seg{u.q0, u.nq, u.k0, u.nk};
                 const int tok0 = u.tok0 + tile * TT;
-                vis = packed_visible(seg, min(tok0 + row / a.group, u.nq - 1), a.causal);
+                vis = packed_visible(seg, min(tok0 + row_tok, u.nq - 1), a.causal);
                 vis_all = packed_visible(seg, tok0, a.causal);
                 vis_end = packed_visible(seg, min(tok0 + TT, u.nq) - 1, a.causal);
+                real = row_tok < TT && tok0 + row_tok < u.nq;
+                to = (bf16*)a.out + (long long)(u.q0 + tok0 + row_tok) * a.out_stride + u.kv_head * a.group * D + head_at;
                 if (u.blocks0 < 0) break;
             }
             float m = -INFINITY;
@@ -392,13 +400,6 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 upk2(add2(sum0, sum1), x, y);
                 inv = x + y == 0.f ? 0.f : 1.f / (x + y);
             }
-            // read again: the loop above needs the registers
-            const volatile PtUnit& u = ctl.units[n % PT_UNITS];
-            const int row_tok = row / a.group, tok = u.tok0 + tile * TT + row_tok;
-            const bool real = row_tok < TT && tok < u.nq;
-            bf16* to = (bf16*)a.out + (long long)(u.q0 + tok) * a.out_stride + (u.kv_head * a.group + row % a.group) * D;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(ctl.unit_empty[n % PT_UNITS]));
 #pragma unroll
             for (int k = 0; k < D; k += 32) {
                 uint32_t o[32];
@@ -411,9 +412,16 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
-                if (real)
+                if (real && sectors) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                                     ::"l"(to + k + 2 * e), "r"(o[e]), "r"(o[e + 1]), "r"(o[e + 2]), "r"(o[e + 3]), "r"(o[e + 4]), "r"(o[e + 5]), "r"(o[e + 6]), "r"(o[e + 7])
+                                     : "memory");
+                } else if (real) {
 #pragma unroll
                     for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + k + 2 * e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
             }
             // O is in registers before the next unit's first P is announced, and that comes before the product that overwrites it
             tc_fence_before();
@@ -500,15 +508,21 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     umma_commit(bar(ctl.kv_empty[v_slot]));
                     if (s.j + 1 == s.mine) umma_commit(bar(ctl.o_ready[i]));
                 };
+                // whether the K block that comes next in the ring has landed
+                auto arrived = [&]() { return test_wait(bar(ctl.kv_full[kv_next % Lay::KV_SLOTS]), (kv_next / Lay::KV_SLOTS) & 1u) != 0; };
                 Step cur, next;
                 bool more = advance(cur, true);
                 if (more) scores(cur);
                 while (more && ok) {
+                    // The next scores go ahead of this product (the other buffer's has been issued), unless they are another unit's that is not there yet.
                     next = cur;
-                    more = advance(next, false);
+                    const bool same = cur.j + 1 < cur.blocks;
+                    const bool ahead = same || (test_wait(bar(ctl.unit_full[units % PT_UNITS]), (units / PT_UNITS) & 1u) && arrived());
+                    if (!ahead) product(cur);
+                    if (ok) more = advance(next, false);
                     if (!ok) break;
-                    if (more) scores(next);                   // the other buffer's product has been issued
-                    if (ok) product(cur);
+                    if (more) scores(next);
+                    if (ok && ahead) product(cur);
                     cur = next;
                 }
             }
