@@ -21,7 +21,6 @@
 // Units are visited by falling cost, there and back over the CTAs: up to PT_SORTED sequences are ranked by every CTA when it starts (more of
 // them are taken in their own order).
 #include <algorithm>
-#include <type_traits>
 
 #include "f32x2.cuh"
 #include "packed.cuh"
@@ -37,7 +36,7 @@ constexpr int PT_KEYS = 64;                                   // keys of a block
 constexpr int PT_SORTED = 256;                                // sequences up to which a CTA ranks them
 constexpr int PT_UNITS = 4;                                   // units announced ahead
 constexpr int PT_TAILS = 2 * PT_UNITS;                        // barriers of value blocks to be cleared; the loads are at most PT_UNITS units ahead of warp 10
-constexpr int PT_POLY = 1;                                    // of eight pairs of exponentials, those worked out by ex2_poly
+constexpr int PT_POLY = 2;                                    // of eight pairs of exponentials, those worked out by ex2_poly
 constexpr float PT_LAG = 8.f;                                 // log2 of how far a row's terms may exceed 1
 
 template <int D>
@@ -127,33 +126,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 // 2^x of a pair without the special-function unit: x = n + f with n whole and |f| <= 1/2 by adding a large number, 2^f by a cubic (least
-// largest relative error, 2^-13.7; the rounding of P to bf16 is up to 2^-8), 2^n from the exponent bits.  x <= 127; below -126 the result is
-// 2^-126.  A NaN stays one.
+// largest relative error, 2^-13.7; the rounding of P to bf16 is up to 2^-8), 2^n from the exponent bits.  x <= 127; below -126.5 the result is
+// 0.  A NaN stays one.
 __device__ __forceinline__ uint64_t ex2_poly(uint64_t z) {
     constexpr float BIG = 12582912.f + 127.f;                 // 1.5 * 2^23; the last bits of t hold n + 127
     float x0, x1, t0, t1;
     upk2(z, x0, x1);
-    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x0) : "f"(x0));             // -126
-    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x1) : "f"(x1));
+    asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(x0) : "f"(x0));             // -127
+    asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(x1) : "f"(x1));
     const uint64_t x = pk2(x0, x1), t = add2(x, pk2(BIG, BIG)), f = fma2(add2(t, pk2(-BIG, -BIG)), pk2(-1.f, -1.f), x);
     uint64_t p = fma2(f, pk2(0.055171322f, 0.055171322f), pk2(0.24261133f, 0.24261133f));
     p = fma2(p, f, pk2(0.69326109f, 0.69326109f));
     p = fma2(p, f, pk2(0.99992806f, 0.99992806f));
     upk2(t, t0, t1);
     return mul2(p, pk2(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23)));
-}
-// hidden keys, and columns that were not formed, count as -inf
-template <int N>
-__device__ __forceinline__ void hide(uint32_t* v, int lim) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = e < lim ? v[e] : 0xFF800000u;
-}
-template <int N>
-__device__ __forceinline__ float max_of(const uint32_t* v, float m) {
-    float t[4] = {m, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-    for (int e = 0; e < N; e += 2) t[(e >> 1) & 3] = max3(t[(e >> 1) & 3], __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-    return fmaxf(max3(t[0], t[1], t[2]), t[3]);
 }
 // V block as the MN-major B operand of O += P V: 64-wide pieces of the head dim lie one behind the other
 template <int D>
@@ -271,7 +257,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
         uint32_t steps = 0, tiles = 0;                        // blocks, tiles with blocks so far
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
-            int blocks, vis, vis_all, vis_end;                // vis_all: keys that every row sees
+            int blocks, vis, vis_all;                         // vis_all: keys that every row sees
             bool real;
             bf16* to;                                         // this thread's row of the output
             {
@@ -285,7 +271,6 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 const int tok0 = u.tok0 + tile * TT;
                 vis = packed_visible(seg, min(tok0 + row_tok, u.nq - 1), a.causal);
                 vis_all = packed_visible(seg, tok0, a.causal);
-                vis_end = packed_visible(seg, min(tok0 + TT, u.nq) - 1, a.causal);
                 real = row_tok < TT && tok0 + row_tok < u.nq;
                 to = (bf16*)a.out + (long long)(u.q0 + tok0 + row_tok) * a.out_stride + u.kv_head * a.group * D + head_at;
                 if (u.blocks0 < 0) break;
@@ -294,30 +279,24 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             uint64_t sum0 = pk2(0.f, 0.f), sum1 = sum0;
             for (int j = 0; j < blocks; ++j, ++steps) {
                 const uint32_t buffer = steps % 2, t_s = lanes + Lay::s_col(tile, buffer);
-                const int ncols = round16(min(PT_KEYS, vis_end - j * PT_KEYS));
-                // a block whose keys all rows see takes a path without conditions
-                const bool whole = vis_all >= (j + 1) * PT_KEYS;
                 ok = wait_asleep(bar(ctl.s_ready[tile][buffer]), (steps / 2) & 1u, abort_flag, a.status);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t v[PT_KEYS];
-                float top;
-                if (whole) {
-                    tmem_ld32(t_s, v);
-                    tmem_ld32(t_s + 32, v + 32);
-                    tmem_ld_wait();
-                    top = max_of<64>(v, -INFINITY);
-                } else {                                      // by 16 columns, twice
-                    top = -INFINITY;
-#pragma unroll 1
-                    for (int k = 0; k < ncols; k += 16) {
-                        tmem_ld16(t_s + k, v);
-                        tmem_ld_wait();
-                        hide<16>(v, vis - j * PT_KEYS - k);
-                        top = max_of<16>(v, top);
-                    }
+                tmem_ld32(t_s, v);
+                tmem_ld32(t_s + 32, v + 32);
+                tmem_ld_wait();
+                // hidden keys, and columns that were not formed, count as -inf
+                if (vis_all < (j + 1) * PT_KEYS) {
+                    const int lim = vis - j * PT_KEYS;
+#pragma unroll
+                    for (int e = 0; e < PT_KEYS; ++e) v[e] = e < lim ? v[e] : 0xFF800000u;
                 }
+                float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int e = 0; e < PT_KEYS; e += 2) t[(e >> 1) & 3] = max3(t[(e >> 1) & 3], __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+                const float top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
                 if (j == 0) {
                     m = top;
                 } else if (__any_sync(0xFFFFFFFFu, top > m + lag)) {
@@ -342,13 +321,15 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 }
                 const float mc = m == -INFINITY ? 0.f : -m * c;              // a row that sees nothing: all terms 0
                 const uint64_t mc2 = pk2(mc, mc);
-                // 16 scores to eight pairs of terms; POLY: of the eight pairs that many by ex2_poly
-                auto terms = [&](const uint32_t* x16, uint32_t* pk, auto poly) {
+                // P of a piece lies over scores that have been read
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        uint64_t p = fma2(pk2(__uint_as_float(x16[2 * e]), __uint_as_float(x16[2 * e + 1])), c2, mc2);
+                for (int k = 0; k < PT_KEYS; k += 32) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        uint64_t p = fma2(pk2(__uint_as_float(v[k + 2 * e]), __uint_as_float(v[k + 2 * e + 1])), c2, mc2);
                         float x, y;
-                        if (e >= 8 - decltype(poly)::value) {
+                        if ((e & 7) >= 8 - PT_POLY) {
                             p = ex2_poly(p);
                             upk2(p, x, y);
                         } else {
@@ -361,27 +342,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                         else sum0 = add2(sum0, p);
                         pk[e] = pack_bf16(x, y);
                     }
-                };
-                // P of a piece lies over scores that have been read before it is stored
-                if (whole) {
-                    constexpr std::integral_constant<int, PT_POLY> poly;
-#pragma unroll
-                    for (int k = 0; k < PT_KEYS; k += 32) {
-                        uint32_t pk[16];
-                        terms(v + k, pk, poly);
-                        terms(v + k + 16, pk + 8, poly);
-                        tmem_st16(t_s + k / 2, pk);
-                    }
-                } else {
-#pragma unroll 1
-                    for (int k = 0; k < ncols; k += 16) {
-                        tmem_ld16(t_s + k, v);
-                        tmem_ld_wait();
-                        hide<16>(v, vis - j * PT_KEYS - k);
-                        uint32_t pk[8];
-                        terms(v, pk, std::integral_constant<int, 0>());
-                        tmem_st8(t_s + k / 2, pk);
-                    }
+                    tmem_st16(t_s + k / 2, pk);
                 }
                 tmem_st_wait();
                 tc_fence_before();
