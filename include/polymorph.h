@@ -28,6 +28,7 @@
 #ifndef POLYMORPH_H_
 #define POLYMORPH_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -473,6 +474,8 @@ typedef struct {
     int32_t* status_out;                  /* dev int32 or NULL: cleared by the call; PM_ERR_ARG if a sequence's offsets or length are
                                              malformed, lie outside the buffers or exceed max_q / max_kv (the sequence is skipped, its
                                              rows of out left as they were), PM_ERR_TIMEOUT if a bounded wait expired */
+    void* workspace;                      /* dev, 16-byte aligned, or NULL; see pm_attention_packed_workspace  */
+    size_t workspace_bytes;
 } pm_packed_attention;
 
 #define PM_PACKED_MAX_SEQS 4096
@@ -480,6 +483,12 @@ typedef struct {
 /* Errors: PM_ERR_ARG (NULL, ranges, alignment), PM_ERR_CAPACITY (n_seqs, heads / kv_heads, kv_heads > 65535, max_q * heads / kv_heads >= 2^30),
  * PM_ERR_CUDA.  Nothing is launched on error. */
 int pm_attention_packed(const pm_packed_attention* args, void* cuda_stream);
+
+/* Host function (needs no GPU; n_sms: multiprocessors of the one that will run the call): bytes of workspace with which the call's few rows
+ * share a long history among all of the GPU; 0 for most calls.  With less, or none, the call takes up to eight CTAs per 16 rows of a K/V head
+ * (48 against 14 us for one token of 16 heads over 32000 keys of 4 heads of 128).  The contents need not be kept; two calls that may overlap
+ * -- on different streams, or in graphs replayed side by side -- need a workspace each. */
+int pm_attention_packed_workspace(const pm_packed_attention* args, int n_sms, size_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -24,7 +24,7 @@ EXPORTS = [
     "pm_select_static", "pm_metrics_reset", "pm_metrics_read", "pm_status", "pm_last_error", "pm_launch_count", "pm_set_graphs", "pm_set_small_batch_kernel", "pm_profile_enable", "pm_profile_read", "pm_plan_stats", "pm_linear_create", "pm_linear_register",
     "pm_linear_forward", "pm_linear_status", "pm_linear_last_error", "pm_linear_destroy",
     "pm_layernorm", "pm_attention", "pm_selftest_wait_timeout", "pm_linear_kernel", "pm_cooccurrence", "pm_build_contexts", "pm_intra_coherence",
-    "pm_rope_init", "pm_rope", "pm_qk_norm_rope", "pm_attention_packed",
+    "pm_rope_init", "pm_rope", "pm_qk_norm_rope", "pm_attention_packed", "pm_attention_packed_workspace",
 ]
 
 
@@ -86,7 +86,7 @@ class pm_packed_attention(C.Structure):
                 [(n, C.c_longlong) for n in ("q_stride", "k_stride", "v_stride", "out_stride")] +
                 [(n, C.c_void_p) for n in ("q_offsets", "kv_offsets", "kv_lengths")] +
                 [(n, C.c_int) for n in ("q_rows", "kv_rows", "n_seqs", "max_q", "max_kv", "heads", "kv_heads", "head_dim", "causal")] +
-                [("scale", C.c_float), ("dtype", C.c_int), ("status_out", C.c_void_p)])
+                [("scale", C.c_float), ("dtype", C.c_int), ("status_out", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)])
 
 
 _lib = None
@@ -143,6 +143,7 @@ def load():
     lib.pm_rope.argtypes = [vp, C.c_longlong, vp, C.c_longlong, vp, ip, ip, vp, ip, vp]
     lib.pm_qk_norm_rope.argtypes = [vp, vp]
     lib.pm_attention_packed.argtypes = [vp, vp]
+    lib.pm_attention_packed_workspace.argtypes = [vp, ip, C.POINTER(C.c_size_t)]
     _lib = lib
     return lib
 
@@ -579,6 +580,24 @@ def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_be
         raise PolymorphError(rc, where)
 
 
+LONG_HISTORY = 4096            # keys below which no call has a use for a workspace
+
+
+def _lend_workspace(lib, args, like, stream):
+    """Memory of torch's for the time of the call on its stream."""
+    import torch
+    need = C.c_size_t(0)
+    sms = torch.cuda.get_device_properties(like.device).multi_processor_count
+    rc = lib.pm_attention_packed_workspace(C.byref(args), sms, C.byref(need))
+    if rc != PM_OK:
+        raise PolymorphError(rc, "pm_attention_packed_workspace")
+    if need.value:
+        space = torch.empty(need.value, dtype=torch.uint8, device=like.device)
+        if stream is not None:
+            space.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream)))
+        args.workspace, args.workspace_bytes = space.data_ptr(), need.value
+
+
 def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offsets=None, kv_lengths=None, causal=False, scale=None, status=None,
                      stream=None):
     """pm_attention_packed: q, out = torch CUDA [rows, heads, head_dim], k, v = [kv rows, kv_heads, head_dim]; q_offsets = torch CUDA int32
@@ -600,6 +619,8 @@ def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offset
         _ints_of(where, "kv_lengths", kv_lengths, (n,))
     args = pm_packed_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(out), qs, ks, vs, os_, _ptr(q_offsets), _ptr(kv_offsets), _ptr(kv_lengths), rows, kv_rows, n,
                                int(max_q), int(max_kv), heads, kv_heads, dim, int(bool(causal)), 0.0 if scale is None else scale, dtype, _ptr(status))
+    if dtype == 0 and max_kv >= LONG_HISTORY and max_q * heads <= 64 * kv_heads:
+        _lend_workspace(lib, args, q, stream)
     rc = lib.pm_attention_packed(C.byref(args), _stream_ptr(stream))
     if rc != PM_OK:
         raise PolymorphError(rc, where)

@@ -70,6 +70,7 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
 constexpr int ROWS_WARPS = 4;
 constexpr int ROWS_STAGES = 3;
 constexpr int ROWS_MAX_CLUSTER = 8;
+constexpr int ROWS_SPLIT_KEYS = 64;          // keys of a warp below which a split is not worth its part
 
 template <int D>
 struct RowsSmem {
@@ -81,15 +82,22 @@ struct RowsSmem {
     float m_cta[16], l_cta[16];
 };
 
+// What a split leaves of a row tile for attention_join_kernel, at ((sequence * K/V heads + head) * tiles + tile) * splits + split.
 template <int D>
-__global__ void __launch_bounds__(32 * ROWS_WARPS) attention_rows_kernel(const __grid_constant__ PackedArgs a, int cluster) {
+struct RowsPart {
+    float o[16][D], m[16], l[16];
+};
+
+// cluster: CTAs that share a row tile's keys and join their parts through shared memory.  splits (without clusters): the same through `parts`.
+template <int D>
+__global__ void __launch_bounds__(32 * ROWS_WARPS) attention_rows_kernel(const __grid_constant__ PackedArgs a, int cluster, int splits, RowsPart<D>* parts) {
     constexpr int CH = D / 8;                                           // 16-byte pieces of a row
     using Smem = RowsSmem<D>;
     static_assert(Smem::RING >= 16 * Smem::PART * 4, "a part fits its ring");
     extern __shared__ __align__(128) uint8_t smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, mi = lane >> 3, l7 = lane & 7;
-    const int rank = cluster > 1 ? blockIdx.x % cluster : 0, tile = cluster > 1 ? blockIdx.x / cluster : blockIdx.x;
+    const int share = cluster * splits, rank = blockIdx.x % share, tile = blockIdx.x / share;
     const int h = blockIdx.y;
     dep_release();
     dep_wait();
@@ -116,7 +124,7 @@ __global__ void __launch_bounds__(32 * ROWS_WARPS) attention_rows_kernel(const _
     const uint32_t ring = smem_u32(sm.ring[warp]);
     const bf16* kp = (const bf16*)a.k + (long long)seg.k0 * a.k_stride + h * D;
     const bf16* vp = (const bf16*)a.v + (long long)seg.k0 * a.v_stride + h * D;
-    const int chunks = (k_end + 15) >> 4, step = cluster * ROWS_WARPS;
+    const int chunks = (k_end + 15) >> 4, step = share * ROWS_WARPS;
     auto fetch = [&](int chunk, int stage) {
         const uint32_t ks = ring + (uint32_t)(stage * 2 * 16 * D * 2), vs = ks + 16 * D * 2;
 #pragma unroll
@@ -240,6 +248,13 @@ __global__ void __launch_bounds__(32 * ROWS_WARPS) attention_rows_kernel(const _
                 acc[e + 2] = fmaf(x.z, f, acc[e + 2]); acc[e + 3] = fmaf(x.w, f, acc[e + 3]);
             }
         }
+        if (splits > 1) {
+            RowsPart<D>& part = parts[((size_t)(blockIdx.z * a.kv_heads + h) * (gridDim.x / splits) + tile) * splits + rank];
+#pragma unroll
+            for (int e = 0; e < EACH; e += 4) *reinterpret_cast<float4*>(&part.o[row][c0 + e * 8]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+            if ((threadIdx.x & 7) == 0) { part.m[row] = m; part.l[row] = l; }
+            return;
+        }
         if (cluster == 1) {
             const int r = r0 + row;
             if (r < rows) {
@@ -284,6 +299,55 @@ __global__ void __launch_bounds__(32 * ROWS_WARPS) attention_rows_kernel(const _
             pack(x * inv, y * inv);
     }
     cluster_sync_all();                                                 // nobody leaves while its part is read
+}
+
+// Joins the splits of a row: a CTA per row, the splits in turn over its warps, lanes over the columns (one warp per row took 6 us for 74
+// splits, one read behind the other).
+constexpr int JOIN_WARPS = 8;
+template <int D>
+__global__ void __launch_bounds__(32 * JOIN_WARPS) attention_join_kernel(const __grid_constant__ PackedArgs a, int splits, int tiles, const RowsPart<D>* parts) {
+    constexpr int EACH = D / 32;
+    __shared__ float so[JOIN_WARPS][D], sm[JOIN_WARPS], sl[JOIN_WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y, r = blockIdx.x, tile = r >> 4, row = r & 15;
+    dep_release();
+    dep_wait();
+    const Segment seg = packed_segment(a, blockIdx.z);
+    if (r >= seg.nq * a.group) return;
+    const RowsPart<D>* p = parts + ((size_t)(blockIdx.z * a.kv_heads + h) * tiles + tile) * splits;
+    float m = -INFINITY, l = 0.f, o[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) o[e] = 0.f;
+    for (int k = warp; k < splits; k += JOIN_WARPS) m = fmaxf(m, p[k].m[row]);
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+    for (int k = warp; k < splits; k += JOIN_WARPS) {
+        const float f = ex2(p[k].m[row] - base);
+        l = fmaf(p[k].l[row], f, l);
+#pragma unroll
+        for (int e = 0; e < EACH; e += 2) {
+            const float2 x = *reinterpret_cast<const float2*>(&p[k].o[row][lane * EACH + e]);
+            o[e] = fmaf(x.x, f, o[e]);
+            o[e + 1] = fmaf(x.y, f, o[e + 1]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < EACH; e += 2) *reinterpret_cast<float2*>(&so[warp][lane * EACH + e]) = make_float2(o[e], o[e + 1]);
+    if (lane == 0) { sm[warp] = m; sl[warp] = l; }
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float top = sm[0];
+#pragma unroll
+    for (int w = 1; w < JOIN_WARPS; ++w) top = fmaxf(top, sm[w]);
+    const float to = top == -INFINITY ? 0.f : top;
+    float x = 0.f, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) {
+        const float f = ex2(sm[w] - to);
+        sum = fmaf(sl[w], f, sum);
+        x = fmaf(so[w][threadIdx.x], f, x);
+    }
+    ((bf16*)a.out)[(long long)(seg.q0 + r / a.group) * a.out_stride + (h * a.group + r % a.group) * D + threadIdx.x] =
+        __float2bfloat16_rn(sum == 0.f ? 0.f : x / sum);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -464,21 +528,51 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
     cluster_sync_all();
 }
 
-// CTAs that share the keys of a row tile: while the grid leaves room for them and each still has `least` keys
+// CTAs that share the keys of a row tile: while the grid leaves room for them and each still has `least` keys; and of long histories, whose
+// lengths may differ, up to eight times as many CTAs as run at once, each with ROWS_EVEN_KEYS still, so that they end together (48 streams of
+// up to 8192 keys: 133 us with a CTA each, 126 with two, 118 with four)
+constexpr int ROWS_EVEN_KEYS = 512;
 int key_split(long long ctas, long long slots, int max_kv, int least) {
     int c = 1;
-    while (c < ROWS_MAX_CLUSTER && ctas * c * 2 <= slots && (long long)max_kv >= 2ll * c * least) c *= 2;
+    while (c < ROWS_MAX_CLUSTER && ((ctas * c * 2 <= slots && (long long)max_kv >= 2ll * c * least) ||
+                                    (ctas * c * 2 <= 8 * slots && (long long)max_kv >= 2ll * c * ROWS_EVEN_KEYS)))
+        c *= 2;
     return c;
 }
 
-template <int D>
-cudaError_t launch_rows(const Launch& L, const PackedArgs& a, int n_sms) {
+// How the keys of a row tile are shared: a cluster joins in shared memory, up to eight CTAs; where even those leave most of the GPU idle and
+// there is a workspace, any number of CTAs leave their parts there and a second kernel joins them.
+struct RowsForm { int tiles, cluster, splits; };
+RowsForm rows_form(const PackedArgs& a, int n_sms) {
     const int tiles = (int)(((long long)a.max_q * a.group + 15) / 16);
-    const int cluster = key_split((long long)tiles * a.kv_heads * a.n_seqs, 2ll * n_sms, a.max_kv, 16 * ROWS_WARPS);
+    const long long ctas = (long long)tiles * a.kv_heads * a.n_seqs, slots = 2ll * n_sms;
+    RowsForm f = {tiles, key_split(ctas, slots, a.max_kv, 16 * ROWS_WARPS), 1};
+    if (f.cluster == ROWS_MAX_CLUSTER && ctas * f.cluster * 2 <= slots) {
+        const long long splits = std::min(slots / ctas, (long long)a.max_kv / (ROWS_SPLIT_KEYS * ROWS_WARPS));
+        if (splits >= 2 * ROWS_MAX_CLUSTER) f.splits = (int)splits;
+    }
+    return f;
+}
+size_t rows_workspace(const PackedArgs& a, int head_dim, const RowsForm& f) {
+    if (f.splits == 1) return 0;
+    return (size_t)a.n_seqs * a.kv_heads * f.tiles * f.splits * (head_dim == 64 ? sizeof(RowsPart<64>) : sizeof(RowsPart<128>));
+}
+
+template <int D>
+cudaError_t launch_rows(const Launch& L, const PackedArgs& a, int n_sms, void* workspace, size_t bytes) {
+    RowsForm f = rows_form(a, n_sms);
+    if (!workspace || bytes < rows_workspace(a, D, f)) f.splits = 1;
+    if (f.splits > 1) f.cluster = 1;
+    RowsPart<D>* parts = (RowsPart<D>*)workspace;
     static SmemGrant grant;
     if (cudaError_t e = grant.ensure(attention_rows_kernel<D>, (int)sizeof(RowsSmem<D>)); e != cudaSuccess) return e;
     ProfScope ps(L, KC_ATTENTION);
-    cudaError_t e = launch_overlapped(L, attention_rows_kernel<D>, dim3(tiles * cluster, a.kv_heads, a.n_seqs), 32 * ROWS_WARPS, sizeof(RowsSmem<D>), cluster, a, cluster);
+    cudaError_t e = launch_overlapped(L, attention_rows_kernel<D>, dim3(f.tiles * f.cluster * f.splits, a.kv_heads, a.n_seqs), 32 * ROWS_WARPS, sizeof(RowsSmem<D>),
+                                      f.cluster, a, f.cluster, f.splits, parts);
+    BUMP(L);
+    if (e != cudaSuccess || f.splits == 1) return e;
+    e = launch_overlapped(L, attention_join_kernel<D>, dim3(a.max_q * a.group, a.kv_heads, a.n_seqs),
+                          32 * JOIN_WARPS, 0, 1, a, f.splits, f.tiles, (const RowsPart<D>*)parts);
     BUMP(L);
     return e;
 }
@@ -502,29 +596,26 @@ bool heads_ok(const void* p, long long stride, int heads, int dim, int dtype) {
 
 }  // namespace
 
-extern "C" int pm_attention_packed(const pm_packed_attention* p, void* cuda_stream) {
+namespace {
+
+bool few_rows(const PackedArgs& a) { return a.kv_rows == 0 || (long long)a.max_q * a.group <= PACKED_FEW_ROWS; }
+
+// Checks everything the host can see; PM_OK with nothing to do leaves a.n_seqs 0.
+int packed_args(const pm_packed_attention* p, PackedArgs& a) {
     if (!p || p->q_rows < 0 || p->kv_rows < 0 || p->n_seqs < 0 || p->max_q < 0 || p->max_kv < 0 || p->heads <= 0 || p->kv_heads <= 0 ||
         p->heads % p->kv_heads || (p->head_dim != 64 && p->head_dim != 128) || (p->dtype != 0 && p->dtype != 1) || !(p->scale >= 0.f) || !isfinite(p->scale))
         return PM_ERR_ARG;
     if (p->n_seqs > PM_PACKED_MAX_SEQS || p->heads / p->kv_heads > PM_PACKED_MAX_GROUP || p->kv_heads > 65535 ||
         (long long)std::min(p->max_q, p->q_rows) * (p->heads / p->kv_heads) > INT32_MAX / 2)
         return PM_ERR_CAPACITY;
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    const bool work = p->n_seqs > 0 && p->q_rows > 0 && p->max_q > 0;
-    if (work) {
-        if (!heads_ok(p->q, p->q_stride, p->heads, p->head_dim, p->dtype) || !heads_ok(p->out, p->out_stride, p->heads, p->head_dim, p->dtype) ||
-            !p->q_offsets || (p->kv_lengths && !p->kv_offsets))
-            return PM_ERR_ARG;
-        if (p->kv_rows > 0 && (!heads_ok(p->k, p->k_stride, p->kv_heads, p->head_dim, p->dtype) ||
-                               !heads_ok(p->v, p->v_stride, p->kv_heads, p->head_dim, p->dtype)))
-            return PM_ERR_ARG;
-    }
-    int dev = 0, n_sms = 0;
-    if (const int rc = stream_device(st, &dev); rc != PM_OK) return rc;
-    if (p->status_out && cudaMemsetAsync(p->status_out, 0, sizeof(int32_t), st) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
-    if (!work) return PM_OK;
-    if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
-    PackedArgs a = {};
+    a = PackedArgs{};
+    if (p->n_seqs == 0 || p->q_rows == 0 || p->max_q == 0) return PM_OK;
+    if (!heads_ok(p->q, p->q_stride, p->heads, p->head_dim, p->dtype) || !heads_ok(p->out, p->out_stride, p->heads, p->head_dim, p->dtype) ||
+        !p->q_offsets || (p->kv_lengths && !p->kv_offsets) || ((uintptr_t)p->workspace & 15))
+        return PM_ERR_ARG;
+    if (p->kv_rows > 0 && (!heads_ok(p->k, p->k_stride, p->kv_heads, p->head_dim, p->dtype) ||
+                           !heads_ok(p->v, p->v_stride, p->kv_heads, p->head_dim, p->dtype)))
+        return PM_ERR_ARG;
     a.q = p->q; a.k = p->k; a.v = p->v; a.out = p->out;
     a.q_stride = p->q_stride; a.k_stride = p->k_stride; a.v_stride = p->v_stride; a.out_stride = p->out_stride;
     a.q_offsets = p->q_offsets; a.kv_offsets = p->kv_offsets; a.kv_lengths = p->kv_lengths;
@@ -532,6 +623,30 @@ extern "C" int pm_attention_packed(const pm_packed_attention* p, void* cuda_stre
     a.max_q = std::min(p->max_q, p->q_rows); a.max_kv = std::min(p->max_kv, p->kv_rows);
     a.heads = p->heads; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads; a.causal = p->causal != 0;
     a.c = (p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
+    return PM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pm_attention_packed_workspace(const pm_packed_attention* p, int n_sms, size_t* bytes) {
+    PackedArgs a;
+    if (!bytes || n_sms <= 0) return PM_ERR_ARG;
+    if (const int rc = packed_args(p, a); rc != PM_OK) return rc;
+    *bytes = a.n_seqs > 0 && p->dtype == 0 && few_rows(a) ? rows_workspace(a, p->head_dim, rows_form(a, n_sms)) : 0;
+    return PM_OK;
+}
+
+int pm_attention_packed(const pm_packed_attention* p, void* cuda_stream) {
+    PackedArgs a;
+    if (const int rc = packed_args(p, a); rc != PM_OK) return rc;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    int dev = 0, n_sms = 0;
+    if (const int rc = stream_device(st, &dev); rc != PM_OK) return rc;
+    if (p->status_out && cudaMemsetAsync(p->status_out, 0, sizeof(int32_t), st) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (a.n_seqs == 0) return PM_OK;
+    if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
     a.status = p->status_out;
     if (!a.status) {
         void* word = nullptr;
@@ -546,10 +661,12 @@ extern "C" int pm_attention_packed(const pm_packed_attention* p, void* cuda_stre
         const bool few = (long long)a.max_q * a.group <= 16;
         e = p->head_dim == 64 ? (few ? launch_f32<64, 16>(L, a, n_sms) : launch_f32<64, 64>(L, a, n_sms))
                               : (few ? launch_f32<128, 16>(L, a, n_sms) : launch_f32<128, 64>(L, a, n_sms));
-    } else if (a.kv_rows > 0 && (long long)a.max_q * a.group > PACKED_FEW_ROWS) {
-        e = launch_packed_tc(L, a, p->head_dim, n_sms);
+    } else if (few_rows(a)) {
+        e = p->head_dim == 64 ? launch_rows<64>(L, a, n_sms, p->workspace, p->workspace_bytes) : launch_rows<128>(L, a, n_sms, p->workspace, p->workspace_bytes);
     } else {
-        e = p->head_dim == 64 ? launch_rows<64>(L, a, n_sms) : launch_rows<128>(L, a, n_sms);
+        e = launch_packed_tc(L, a, p->head_dim, n_sms);
     }
     return e == cudaSuccess ? PM_OK : PM_ERR_CUDA;
 }
+
+}  // extern "C"
