@@ -8,14 +8,16 @@
 // at any 32-bit position (a 32-bit product of position and frequency is off by 0.06 rad at position 10^6).  sincospi of that
 // fraction needs no argument reduction.
 //
-// Bound by memory: every element is read and written once.  A thread holds 16 elements of a head -- the eight pairs
-// whose angles they share -- as two 16-byte pieces (bf16): elements 8u.. and rot/2 + 8u.. (half layout) or 16u.. (interleaved,
-// and what lies behind rot).  A warp takes a row: LP lanes a head, 32 / LP heads at once.  The lanes with the same u share
-// the work on its eight angles and pass them on by shuffles; they are used for all heads of the row.
+// Every element is read and written once.  A thread holds 16 elements of a head as 16-byte pieces (two of bf16, four of fp32) that lie
+// side by side with the neighbouring threads', so that each load and store of a warp covers whole lines: with half layout the pairs of the
+// rotated part, or a quarter or half of the rest; interleaved, a quarter or half of the head from its place on.  A warp takes a row: LP lanes
+// a head, 32 / LP heads at once.  The lanes of the same place share the work on its eight angles and pass them on by shuffles; they
+// are used for all heads of the row.
 #include <math.h>
 
 #include <algorithm>
 
+#include "f32x2.cuh"
 #include "tcgen05_ptx.cuh"
 
 #define BUMP(L) do { if ((L).launches) ++*(L).launches; } while (0)
@@ -24,6 +26,10 @@ namespace {
 
 constexpr int ROT_THREADS = 128;
 constexpr int ROT_WARPS = ROT_THREADS / 32;
+constexpr int ROT_RESIDENT = 4;                // CTAs of an SM
+// heads of a warp whose loads are issued together, ahead of the angles
+template <typename T, bool NORMS>
+constexpr int ROT_BATCH = sizeof(T) == 4 ? 2 : NORMS ? 3 : 4;
 
 struct RotArgs {
     const void *x[2];              // queries, keys (the rotation alone: one of them)
@@ -32,7 +38,7 @@ struct RotArgs {
     int heads[2];
     const float *gamma[2], *beta[2];
     int per_head;                  // gamma and beta of each head, else shared by all
-    float eps;
+    float eps, inv_dim;
     const int* positions;          // [rows, axes], or null: no rotation
     int rows, units, rot_units;    // units: 16-element pieces of a head; of the rotated part
     int steps;                     // warp iterations over the heads of a row
@@ -40,56 +46,89 @@ struct RotArgs {
     pm_rope_table table;
 };
 
-struct __align__(16) Bf16x8 { __nv_bfloat162 v[4]; };
-
-__device__ __forceinline__ void load8(const bf16* p, float* v) {
-    const uint4 r = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+// A 16-byte piece as packed pairs: of every four elements lo holds 0 and 2, hi 1 and 3.  So the two of an interleaved pair stand at the same
+// place of lo and hi, and the arithmetic runs on two results per instruction in either layout (one at a time it takes twice the cycles of the
+// floating-point unit).
+template <typename T> struct Piece;
+template <> struct Piece<bf16> {
+    static constexpr int ELEMENTS = 8, WORDS = 2;             // WORDS: of lo, of hi
+    uint4 r;
+    __device__ __forceinline__ void load(const bf16* p) { r = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void unpack(uint64_t* lo, uint64_t* hi) const {           // a bf16 is the upper half of its 32-bit value
+        lo[0] = pk2(__uint_as_float(r.x << 16), __uint_as_float(r.y << 16));
+        hi[0] = pk2(__uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y & 0xFFFF0000u));
+        lo[1] = pk2(__uint_as_float(r.z << 16), __uint_as_float(r.w << 16));
+        hi[1] = pk2(__uint_as_float(r.z & 0xFFFF0000u), __uint_as_float(r.w & 0xFFFF0000u));
+    }
+    static __device__ __forceinline__ void store(bf16* p, const uint64_t* lo, const uint64_t* hi) {
+        float a[4], b[4];
+        upk2(lo[0], a[0], a[1]); upk2(lo[1], a[2], a[3]);
+        upk2(hi[0], b[0], b[1]); upk2(hi[1], b[2], b[3]);
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(a[0], b[0]), pack_bf16(a[1], b[1]), pack_bf16(a[2], b[2]), pack_bf16(a[3], b[3]));
+    }
+};
+template <> struct Piece<float> {
+    static constexpr int ELEMENTS = 4, WORDS = 1;
+    float4 r;
+    __device__ __forceinline__ void load(const float* p) { r = *reinterpret_cast<const float4*>(p); }
+    __device__ __forceinline__ void unpack(uint64_t* lo, uint64_t* hi) const { lo[0] = pk2(r.x, r.z); hi[0] = pk2(r.y, r.w); }
+    static __device__ __forceinline__ void store(float* p, const uint64_t* lo, const uint64_t* hi) {
+        float4 a;
+        upk2(lo[0], a.x, a.z); upk2(hi[0], a.y, a.w);
+        *reinterpret_cast<float4*>(p) = a;
+    }
+};
+// as many 32-bit weights as a piece has elements
+template <typename T>
+__device__ __forceinline__ void load_weights(const float* p, uint64_t* lo, uint64_t* hi) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {                       // a bf16 is the upper half of its 32-bit value
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    for (int i = 0; i < Piece<T>::WORDS; ++i) {
+        Piece<float> w;
+        w.load(p + 4 * i);
+        w.unpack(lo + i, hi + i);
     }
 }
-__device__ __forceinline__ void load8(const float* p, float* v) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void store8(bf16* p, const float* v) {
-    Bf16x8 o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o.v[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&o);
-}
-__device__ __forceinline__ void store8(float* p, const float* v) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ float sum2(uint64_t x) {
+    float a, b;
+    upk2(x, a, b);
+    return a + b;
 }
 
 enum { NORM_NONE = 0, NORM_RMS = 1, NORM_LAYER = 2 };
 
 template <typename T, int NORM, int LP>
-__global__ void __launch_bounds__(ROT_THREADS) rotate_kernel(const __grid_constant__ RotArgs a) {
+__global__ void __launch_bounds__(ROT_THREADS, ROT_RESIDENT) rotate_kernel(const __grid_constant__ RotArgs a) {
     constexpr int HW = 32 / LP;                          // heads of a warp iteration
     constexpr int PPL = HW >= 8 ? 1 : 8 / HW;            // angles a lane works out
+    constexpr int BATCH = ROT_BATCH<T, NORM != NORM_NONE>;
+    constexpr int PIECES = 16 / Piece<T>::ELEMENTS, WORDS = Piece<T>::WORDS;
     const int lane = threadIdx.x & 31, u = lane % LP, slot = lane / LP;
-    const bool used = u < a.units, turns = u < a.rot_units && a.positions;
-    const bool interleaved = a.table.interleaved != 0;
-    // offsets of the two 8-element pieces in a head
-    const int at0 = u >= a.rot_units || interleaved ? 16 * u : 8 * u;
-    const int at1 = u >= a.rot_units || interleaved ? at0 + 8 : a.rot_units * 8 + 8 * u;
-    const int dim = a.units * 16;
+    const bool used = u < a.units, interleaved = a.table.interleaved != 0;
+    const int dim = a.units * 16, rot = a.positions ? a.rot_units * 16 : 0;
     const int all = a.heads[0] + a.heads[1];
     const float amplitude = a.table.amplitude;
-    // this lane's angles: pair 8u + its own of the eight, on axis 0 or 1
+    // this thread's pieces: of the whole head, or with half layout of the rotated part or of the rest
+    const bool split = !interleaved && rot > 0, front = u < a.rot_units;
+    const int base = split && !front ? rot : 0, size = !split ? dim : front ? rot : dim - rot, place = split && !front ? u - a.rot_units : u;
+    int at[PIECES];
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) at[k] = base + Piece<T>::ELEMENTS * place + k * (size / PIECES);
+    // element of lo[k]'s first half (lo holds it and the one two behind, hi the next ones)
+    auto element = [&](int k) { return base + Piece<T>::ELEMENTS * place + (k / WORDS) * (size / PIECES) + 4 * (k % WORDS); };
+    bool turns[4];                                       // whether lo[k] and hi[k] are turned
+#pragma unroll
+    for (int k = 0; k < 4; ++k) turns[k] = used && rot > 0 && element(k) < rot;
+    // The thread's eight angles, c[x / 2] half x % 2: interleaved, the pairs of lo[k] and hi[k] in order; with half layout those of lo[0], lo[1],
+    // hi[0], hi[1], whose partners are lo[2] and so on.  This lane works out PPL of them.
     unsigned long long step[PPL];
     int axis[PPL];
-    const int pairs = a.rot_units * 8, own = (slot * PPL) & 7;
 #pragma unroll
     for (int i = 0; i < PPL; ++i) {
-        const int p = 8 * u + own + i;
-        step[i] = turns ? a.table.step[p] : 0ull;
-        axis[i] = a.table.axes == 2 && 2 * p >= pairs ? 1 : 0;
+        const int x = ((slot * PPL) & 7) + i, k = x >> 1;
+        const int pair = interleaved ? element(k) / 2 + (x & 1) : element(k & 1) + 2 * (x & 1) + (k >> 1);
+        const bool turned = used && rot > 0 && pair < rot / 2;
+        step[i] = turned ? a.table.step[pair] : 0ull;
+        axis[i] = a.table.axes == 2 && 4 * pair >= rot ? 1 : 0;
     }
     const long long tasks = (long long)a.rows * a.parts, stride = (long long)gridDim.x * ROT_WARPS;
     dep_release();
@@ -97,96 +136,116 @@ __global__ void __launch_bounds__(ROT_THREADS) rotate_kernel(const __grid_consta
     for (long long task = (long long)blockIdx.x * ROT_WARPS + (threadIdx.x >> 5); task < tasks; task += stride) {
         const long long row = a.parts == 1 ? task : task / a.parts;
         const int part = a.parts == 1 ? 0 : (int)(task - row * a.parts);
-        float c[8], s[8];
-        if (a.positions) {
-            float mc[PPL], ms[PPL];
-#pragma unroll
-            for (int i = 0; i < PPL; ++i) {
-                const long long p = a.positions[row * a.table.axes + axis[i]];
-                const int turn = (int)(((unsigned long long)p * step[i]) >> 32);         // of 2^32 to a turn, signed
-                sincospif((float)turn * 4.656612873077393e-10f, &ms[i], &mc[i]);         // 2^-31: in half turns
-                mc[i] *= amplitude;
-                ms[i] *= amplitude;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int from = (i / PPL) * LP + u;
-                c[i] = __shfl_sync(0xFFFFFFFFu, mc[i % PPL], from);
-                s[i] = __shfl_sync(0xFFFFFFFFu, ms[i % PPL], from);
-            }
-        }
         const int first = a.steps * part / a.parts, end = a.steps * (part + 1) / a.parts;
-#pragma unroll 2
-        for (int it = first; it < end; ++it) {
-            const int head = it * HW + slot;
-            const int w = head >= a.heads[0] ? 1 : 0, h = w ? head - a.heads[0] : head;
-            const bool live = used && head < all;
-            float v[16];
+        const T* xr[2] = {(const T*)a.x[0] + row * a.x_stride[0], (const T*)a.x[1] + row * a.x_stride[1]};
+        T* yr[2] = {(T*)a.y[0] + row * a.y_stride[0], (T*)a.y[1] + row * a.y_stride[1]};
+        uint64_t c[4], s[4], ns[4];                      // cos, sin, -sin
+        for (int it0 = first; it0 < end; it0 += BATCH) {
+            Piece<T> raw[BATCH][PIECES];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = 0.f;
-            if (live) {
-                const T* x = (const T*)a.x[w] + row * a.x_stride[w] + (long long)h * dim;
-                load8(x + at0, v);
-                load8(x + at1, v + 8);
+            for (int i = 0; i < BATCH; ++i) {
+                const int head = (it0 + i) * HW + slot, w = head >= a.heads[0] ? 1 : 0, h = w ? head - a.heads[0] : head;
+                const T* x = (w ? xr[1] : xr[0]) + h * dim;
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k) {
+                    raw[i][k] = Piece<T>{};
+                    if (used && head < all && it0 + i < end) raw[i][k].load(x + at[k]);
+                }
             }
-            if (NORM != NORM_NONE) {
-                float mean = 0.f, sum = 0.f;
-                if (NORM == NORM_LAYER) {
+            if (it0 == first && rot > 0) {
+                float mc[PPL], ms[PPL];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) mean += v[i];
+                for (int i = 0; i < PPL; ++i) {
+                    const long long p = a.positions[row * a.table.axes + axis[i]];
+                    const int turn = (int)(((unsigned long long)p * step[i]) >> 32);     // of 2^32 to a turn, signed
+                    sincospif((float)turn * 4.656612873077393e-10f, &ms[i], &mc[i]);     // 2^-31: in half turns
+                    mc[i] *= amplitude;
+                    ms[i] *= amplitude;
+                }
+                float fc[8], fs[8];
 #pragma unroll
-                    for (int m = 1; m < LP; m <<= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, m);
-                    mean /= (float)dim;
-                    if (used)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] -= mean;
+                for (int i = 0; i < 8; ++i) {
+                    const int from = (i / PPL) * LP + u;
+                    fc[i] = __shfl_sync(0xFFFFFFFFu, mc[i % PPL], from);
+                    fs[i] = __shfl_sync(0xFFFFFFFFu, ms[i % PPL], from);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
+                for (int k = 0; k < 4; ++k) {
+                    c[k] = pk2(fc[2 * k], fc[2 * k + 1]);
+                    s[k] = pk2(fs[2 * k], fs[2 * k + 1]);
+                    ns[k] = s[k] ^ 0x8000000080000000ull;
+                }
+            }
 #pragma unroll
-                for (int m = 1; m < LP; m <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
-                const float inv = 1.f / sqrtf(sum / (float)dim + a.eps);
-                if (live) {
-                    const float* g = a.gamma[w] + (a.per_head ? h * dim : 0);
-                    float t[8];
+            for (int i = 0; i < BATCH; ++i) {
+                if (it0 + i >= end) break;
+                const int head = (it0 + i) * HW + slot, w = head >= a.heads[0] ? 1 : 0, h = w ? head - a.heads[0] : head;
+                const bool live = used && head < all;
+                uint64_t lo[4], hi[4];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        load8(g + (k ? at1 : at0), t);
+                for (int k = 0; k < PIECES; ++k) raw[i][k].unpack(lo + k * WORDS, hi + k * WORDS);
+                if (NORM != NORM_NONE) {
+                    uint64_t acc = 0ull;
+                    if (NORM == NORM_LAYER) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[8 * k + i] *= inv * t[i];
+                        for (int k = 0; k < 4; ++k) acc = add2(acc, add2(lo[k], hi[k]));
+                        float mean = sum2(acc);
+#pragma unroll
+                        for (int m = 1; m < LP; m <<= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, m);
+                        mean = used ? -mean * a.inv_dim : 0.f;
+                        const uint64_t m2 = pk2(mean, mean);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) { lo[k] = add2(lo[k], m2); hi[k] = add2(hi[k], m2); }
+                        acc = 0ull;
                     }
-                    if (NORM == NORM_LAYER && a.beta[w]) {
-                        const float* b = a.beta[w] + (a.per_head ? h * dim : 0);
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            load8(b + (k ? at1 : at0), t);
+                    for (int k = 0; k < 4; ++k) acc = fma2(hi[k], hi[k], fma2(lo[k], lo[k], acc));
+                    float sum = sum2(acc);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) v[8 * k + i] += t[i];
+                    for (int m = 1; m < LP; m <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
+                    const float inv = rsqrtf(fmaf(sum, a.inv_dim, a.eps));
+                    if (live) {
+                        const float* g = (w ? a.gamma[1] : a.gamma[0]) + (a.per_head ? h * dim : 0);
+                        const uint64_t i2 = pk2(inv, inv);
+                        uint64_t gl[4], gh[4], bl[4] = {0ull, 0ull, 0ull, 0ull}, bh[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+                        for (int k = 0; k < PIECES; ++k) load_weights<T>(g + at[k], gl + k * WORDS, gh + k * WORDS);
+                        if (NORM == NORM_LAYER) {
+                            const float* b = w ? a.beta[1] : a.beta[0];
+                            if (b) {
+                                b += a.per_head ? h * dim : 0;
+#pragma unroll
+                                for (int k = 0; k < PIECES; ++k) load_weights<T>(b + at[k], bl + k * WORDS, bh + k * WORDS);
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            lo[k] = NORM == NORM_LAYER ? fma2(lo[k], mul2(gl[k], i2), bl[k]) : mul2(lo[k], mul2(gl[k], i2));
+                            hi[k] = NORM == NORM_LAYER ? fma2(hi[k], mul2(gh[k], i2), bh[k]) : mul2(hi[k], mul2(gh[k], i2));
                         }
                     }
                 }
-            }
-            if (turns) {
+                auto turn = [](uint64_t& p, uint64_t& q, uint64_t c, uint64_t s, uint64_t ns) {
+                    const uint64_t x = fma2(p, c, mul2(q, ns));
+                    q = fma2(p, s, mul2(q, c));
+                    p = x;
+                };
                 if (interleaved) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float p = v[2 * i], q = v[2 * i + 1];
-                        v[2 * i] = p * c[i] - q * s[i];
-                        v[2 * i + 1] = p * s[i] + q * c[i];
-                    }
-                } else {
+                    for (int k = 0; k < 4; ++k)
+                        if (turns[k]) turn(lo[k], hi[k], c[k], s[k], ns[k]);
+                } else if (turns[0]) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float p = v[i], q = v[8 + i];
-                        v[i] = p * c[i] - q * s[i];
-                        v[8 + i] = p * s[i] + q * c[i];
+                    for (int k = 0; k < 2; ++k) {
+                        turn(lo[k], lo[k + 2], c[k], s[k], ns[k]);
+                        turn(hi[k], hi[k + 2], c[k + 2], s[k + 2], ns[k + 2]);
                     }
                 }
-            }
-            if (live) {
-                T* y = (T*)a.y[w] + row * a.y_stride[w] + (long long)h * dim;
-                store8(y + at0, v);
-                store8(y + at1, v + 8);
+                if (live) {
+                    T* y = (w ? yr[1] : yr[0]) + h * dim;
+#pragma unroll
+                    for (int k = 0; k < PIECES; ++k) Piece<T>::store(y + at[k], lo + k * WORDS, hi + k * WORDS);
+                }
             }
         }
     }
@@ -196,11 +255,11 @@ template <typename T, int NORM, int LP>
 cudaError_t rotate_launch(const Launch& L, RotArgs& a, int n_sms) {
     constexpr int HW = 32 / LP;
     a.steps = (a.heads[0] + a.heads[1] + HW - 1) / HW;
-    // a row to a warp while that fills the GPU (sixteen warps a multiprocessor); fewer rows are cut along their heads
-    const long long want = 16ll * n_sms;
+    // a row to a warp while that fills the GPU; fewer rows are cut along their heads
+    const long long want = (long long)ROT_RESIDENT * ROT_WARPS * n_sms;
     a.parts = (int)std::min<long long>(a.steps, std::max<long long>(1, want / a.rows));
     const long long blocks = ((long long)a.rows * a.parts + ROT_WARPS - 1) / ROT_WARPS;
-    const int grid = (int)std::min<long long>(blocks, 16ll * n_sms);
+    const int grid = (int)std::min<long long>(blocks, (long long)ROT_RESIDENT * n_sms);
     ProfScope ps(L, KC_LAYERNORM);
     const cudaError_t e = launch_overlapped(L, rotate_kernel<T, NORM, LP>, grid, ROT_THREADS, 0, 1, a);
     BUMP(L);
@@ -237,6 +296,7 @@ int rotate(RotArgs& a, int norm, int dtype, void* cuda_stream) {
     int dev = 0, n_sms = 0;
     if (const int rc = stream_device(st, &dev); rc != PM_OK) return rc;
     if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    a.inv_dim = 1.f / (float)(a.units * 16);
     Launch L;
     L.st = st;
     const cudaError_t e = dtype == 0 ? rotate_norm<bf16>(L, a, norm, n_sms) : rotate_norm<float>(L, a, norm, n_sms);
