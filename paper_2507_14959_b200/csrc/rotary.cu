@@ -46,46 +46,60 @@ struct RotArgs {
     pm_rope_table table;
 };
 
-// A 16-byte piece as packed pairs: of every four elements lo holds 0 and 2, hi 1 and 3.  So the two of an interleaved pair stand at the same
-// place of lo and hi, and the arithmetic runs on two results per instruction in either layout (one at a time it takes twice the cycles of the
-// floating-point unit).
-template <typename T> struct Piece;
-template <> struct Piece<bf16> {
-    static constexpr int ELEMENTS = 8, WORDS = 2;             // WORDS: of lo, of hi
+// A 16-byte piece as packed pairs, so that the arithmetic runs on two results per instruction (one at a time it takes twice the cycles of the
+// floating-point unit).  Half layout: elements (0, 1), (2, 3) and so on.  Interleaved (IL): of every four elements (0, 2), then (1, 3), so that the two
+// of a rotated pair stand at the same place of two packed ones.
+template <typename T, bool IL> struct Piece;
+template <bool IL> struct Piece<bf16, IL> {
+    static constexpr int ELEMENTS = 8;
     uint4 r;
     __device__ __forceinline__ void load(const bf16* p) { r = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void unpack(uint64_t* lo, uint64_t* hi) const {           // a bf16 is the upper half of its 32-bit value
-        lo[0] = pk2(__uint_as_float(r.x << 16), __uint_as_float(r.y << 16));
-        hi[0] = pk2(__uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y & 0xFFFF0000u));
-        lo[1] = pk2(__uint_as_float(r.z << 16), __uint_as_float(r.w << 16));
-        hi[1] = pk2(__uint_as_float(r.z & 0xFFFF0000u), __uint_as_float(r.w & 0xFFFF0000u));
+    __device__ __forceinline__ void unpack(uint64_t* v) const {              // a bf16 is the upper half of its 32-bit value
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+            const float a = __uint_as_float(w[k] << 16), b = __uint_as_float(w[k] & 0xFFFF0000u);
+            const float c = __uint_as_float(w[k + 1] << 16), d = __uint_as_float(w[k + 1] & 0xFFFF0000u);
+            v[k] = IL ? pk2(a, c) : pk2(a, b);
+            v[k + 1] = IL ? pk2(b, d) : pk2(c, d);
+        }
     }
-    static __device__ __forceinline__ void store(bf16* p, const uint64_t* lo, const uint64_t* hi) {
-        float a[4], b[4];
-        upk2(lo[0], a[0], a[1]); upk2(lo[1], a[2], a[3]);
-        upk2(hi[0], b[0], b[1]); upk2(hi[1], b[2], b[3]);
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(a[0], b[0]), pack_bf16(a[1], b[1]), pack_bf16(a[2], b[2]), pack_bf16(a[3], b[3]));
+    static __device__ __forceinline__ void store(bf16* p, const uint64_t* v) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+            float a, b, c, d;
+            upk2(v[k], a, b);
+            upk2(v[k + 1], c, d);
+            w[k] = IL ? pack_bf16(a, c) : pack_bf16(a, b);
+            w[k + 1] = IL ? pack_bf16(b, d) : pack_bf16(c, d);
+        }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
-template <> struct Piece<float> {
-    static constexpr int ELEMENTS = 4, WORDS = 1;
+template <bool IL> struct Piece<float, IL> {
+    static constexpr int ELEMENTS = 4;
     float4 r;
     __device__ __forceinline__ void load(const float* p) { r = *reinterpret_cast<const float4*>(p); }
-    __device__ __forceinline__ void unpack(uint64_t* lo, uint64_t* hi) const { lo[0] = pk2(r.x, r.z); hi[0] = pk2(r.y, r.w); }
-    static __device__ __forceinline__ void store(float* p, const uint64_t* lo, const uint64_t* hi) {
-        float4 a;
-        upk2(lo[0], a.x, a.z); upk2(hi[0], a.y, a.w);
-        *reinterpret_cast<float4*>(p) = a;
+    __device__ __forceinline__ void unpack(uint64_t* v) const {
+        v[0] = IL ? pk2(r.x, r.z) : pk2(r.x, r.y);
+        v[1] = IL ? pk2(r.y, r.w) : pk2(r.z, r.w);
+    }
+    static __device__ __forceinline__ void store(float* p, const uint64_t* v) {
+        float a, b, c, d;
+        upk2(v[0], a, b);
+        upk2(v[1], c, d);
+        *reinterpret_cast<float4*>(p) = IL ? make_float4(a, c, b, d) : make_float4(a, b, c, d);
     }
 };
-// as many 32-bit weights as a piece has elements
-template <typename T>
-__device__ __forceinline__ void load_weights(const float* p, uint64_t* lo, uint64_t* hi) {
+// the weights of a piece's N elements, packed alike
+template <int N, bool IL>
+__device__ __forceinline__ void load_weights(const float* p, uint64_t* v) {
 #pragma unroll
-    for (int i = 0; i < Piece<T>::WORDS; ++i) {
-        Piece<float> w;
+    for (int i = 0; i < N / 4; ++i) {
+        Piece<float, IL> w;
         w.load(p + 4 * i);
-        w.unpack(lo + i, hi + i);
+        w.unpack(v + 2 * i);
     }
 }
 __device__ __forceinline__ float sum2(uint64_t x) {
@@ -96,37 +110,35 @@ __device__ __forceinline__ float sum2(uint64_t x) {
 
 enum { NORM_NONE = 0, NORM_RMS = 1, NORM_LAYER = 2 };
 
-template <typename T, int NORM, int LP>
+template <typename T, int NORM, int LP, bool IL>
 __global__ void __launch_bounds__(ROT_THREADS, ROT_RESIDENT) rotate_kernel(const __grid_constant__ RotArgs a) {
     constexpr int HW = 32 / LP;                          // heads of a warp iteration
     constexpr int PPL = HW >= 8 ? 1 : 8 / HW;            // angles a lane works out
     constexpr int BATCH = ROT_BATCH<T, NORM != NORM_NONE>;
-    constexpr int PIECES = 16 / Piece<T>::ELEMENTS, WORDS = Piece<T>::WORDS;
+    constexpr int PE = Piece<T, IL>::ELEMENTS, PIECES = 16 / PE;
     const int lane = threadIdx.x & 31, u = lane % LP, slot = lane / LP;
-    const bool used = u < a.units, interleaved = a.table.interleaved != 0;
+    const bool used = u < a.units;
     const int dim = a.units * 16, rot = a.positions ? a.rot_units * 16 : 0;
     const int all = a.heads[0] + a.heads[1];
     const float amplitude = a.table.amplitude;
     // this thread's pieces: of the whole head, or with half layout of the rotated part or of the rest
-    const bool split = !interleaved && rot > 0, front = u < a.rot_units;
+    const bool split = !IL && rot > 0, front = u < a.rot_units;
     const int base = split && !front ? rot : 0, size = !split ? dim : front ? rot : dim - rot, place = split && !front ? u - a.rot_units : u;
     int at[PIECES];
 #pragma unroll
-    for (int k = 0; k < PIECES; ++k) at[k] = base + Piece<T>::ELEMENTS * place + k * (size / PIECES);
-    // element of lo[k]'s first half (lo holds it and the one two behind, hi the next ones)
-    auto element = [&](int k) { return base + Piece<T>::ELEMENTS * place + (k / WORDS) * (size / PIECES) + 4 * (k % WORDS); };
-    bool turns[4];                                       // whether lo[k] and hi[k] are turned
+    for (int k = 0; k < PIECES; ++k) at[k] = base + PE * place + k * (size / PIECES);
+    // The thread's eight angles, c[x / 2] half x % 2.  Interleaved: of the pairs v[2 k], v[2 k + 1] in order.  Half layout: of v[0] to v[3], whose partners
+    // are v[4] to v[7].  This lane works out PPL of them.
+    bool turns[4];                                       // whether v[2 k], v[2 k + 1] are turned
 #pragma unroll
-    for (int k = 0; k < 4; ++k) turns[k] = used && rot > 0 && element(k) < rot;
-    // The thread's eight angles, c[x / 2] half x % 2: interleaved, the pairs of lo[k] and hi[k] in order; with half layout those of lo[0], lo[1],
-    // hi[0], hi[1], whose partners are lo[2] and so on.  This lane works out PPL of them.
+    for (int k = 0; k < 4; ++k) turns[k] = used && base + PE * place + (4 * k / PE) * (size / PIECES) + 4 * k % PE < rot;
     unsigned long long step[PPL];
     int axis[PPL];
 #pragma unroll
     for (int i = 0; i < PPL; ++i) {
-        const int x = ((slot * PPL) & 7) + i, k = x >> 1;
-        const int pair = interleaved ? element(k) / 2 + (x & 1) : element(k & 1) + 2 * (x & 1) + (k >> 1);
-        const bool turned = used && rot > 0 && pair < rot / 2;
+        const int x = ((slot * PPL) & 7) + i, e = IL ? 2 * x : x;            // the pair's first element among the thread's sixteen
+        const int element = base + PE * place + (e / PE) * (size / PIECES) + e % PE, pair = IL ? element / 2 : element;
+        const bool turned = used && pair < rot / 2;
         step[i] = turned ? a.table.step[pair] : 0ull;
         axis[i] = a.table.axes == 2 && 4 * pair >= rot ? 1 : 0;
     }
@@ -141,14 +153,14 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_RESIDENT) rotate_kernel(const
         T* yr[2] = {(T*)a.y[0] + row * a.y_stride[0], (T*)a.y[1] + row * a.y_stride[1]};
         uint64_t c[4], s[4], ns[4];                      // cos, sin, -sin
         for (int it0 = first; it0 < end; it0 += BATCH) {
-            Piece<T> raw[BATCH][PIECES];
+            Piece<T, IL> raw[BATCH][PIECES];
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
                 const int head = (it0 + i) * HW + slot, w = head >= a.heads[0] ? 1 : 0, h = w ? head - a.heads[0] : head;
                 const T* x = (w ? xr[1] : xr[0]) + h * dim;
 #pragma unroll
                 for (int k = 0; k < PIECES; ++k) {
-                    raw[i][k] = Piece<T>{};
+                    raw[i][k] = Piece<T, IL>{};
                     if (used && head < all && it0 + i < end) raw[i][k].load(x + at[k]);
                 }
             }
@@ -181,25 +193,25 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_RESIDENT) rotate_kernel(const
                 if (it0 + i >= end) break;
                 const int head = (it0 + i) * HW + slot, w = head >= a.heads[0] ? 1 : 0, h = w ? head - a.heads[0] : head;
                 const bool live = used && head < all;
-                uint64_t lo[4], hi[4];
+                uint64_t v[8];
 #pragma unroll
-                for (int k = 0; k < PIECES; ++k) raw[i][k].unpack(lo + k * WORDS, hi + k * WORDS);
+                for (int k = 0; k < PIECES; ++k) raw[i][k].unpack(v + k * PE / 2);
                 if (NORM != NORM_NONE) {
                     uint64_t acc = 0ull;
                     if (NORM == NORM_LAYER) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) acc = add2(acc, add2(lo[k], hi[k]));
+                        for (int k = 0; k < 8; k += 2) acc = add2(acc, add2(v[k], v[k + 1]));
                         float mean = sum2(acc);
 #pragma unroll
                         for (int m = 1; m < LP; m <<= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, m);
                         mean = used ? -mean * a.inv_dim : 0.f;
                         const uint64_t m2 = pk2(mean, mean);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) { lo[k] = add2(lo[k], m2); hi[k] = add2(hi[k], m2); }
+                        for (int k = 0; k < 8; ++k) v[k] = add2(v[k], m2);
                         acc = 0ull;
                     }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc = fma2(hi[k], hi[k], fma2(lo[k], lo[k], acc));
+                    for (int k = 0; k < 8; ++k) acc = fma2(v[k], v[k], acc);
                     float sum = sum2(acc);
 #pragma unroll
                     for (int m = 1; m < LP; m <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
@@ -207,22 +219,19 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_RESIDENT) rotate_kernel(const
                     if (live) {
                         const float* g = (w ? a.gamma[1] : a.gamma[0]) + (a.per_head ? h * dim : 0);
                         const uint64_t i2 = pk2(inv, inv);
-                        uint64_t gl[4], gh[4], bl[4] = {0ull, 0ull, 0ull, 0ull}, bh[4] = {0ull, 0ull, 0ull, 0ull};
+                        uint64_t gw[8], bw[8] = {};
 #pragma unroll
-                        for (int k = 0; k < PIECES; ++k) load_weights<T>(g + at[k], gl + k * WORDS, gh + k * WORDS);
+                        for (int k = 0; k < PIECES; ++k) load_weights<PE, IL>(g + at[k], gw + k * PE / 2);
                         if (NORM == NORM_LAYER) {
                             const float* b = w ? a.beta[1] : a.beta[0];
                             if (b) {
                                 b += a.per_head ? h * dim : 0;
 #pragma unroll
-                                for (int k = 0; k < PIECES; ++k) load_weights<T>(b + at[k], bl + k * WORDS, bh + k * WORDS);
+                                for (int k = 0; k < PIECES; ++k) load_weights<PE, IL>(b + at[k], bw + k * PE / 2);
                             }
                         }
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            lo[k] = NORM == NORM_LAYER ? fma2(lo[k], mul2(gl[k], i2), bl[k]) : mul2(lo[k], mul2(gl[k], i2));
-                            hi[k] = NORM == NORM_LAYER ? fma2(hi[k], mul2(gh[k], i2), bh[k]) : mul2(hi[k], mul2(gh[k], i2));
-                        }
+                        for (int k = 0; k < 8; ++k) v[k] = NORM == NORM_LAYER ? fma2(v[k], mul2(gw[k], i2), bw[k]) : mul2(v[k], mul2(gw[k], i2));
                     }
                 }
                 auto turn = [](uint64_t& p, uint64_t& q, uint64_t c, uint64_t s, uint64_t ns) {
@@ -230,21 +239,18 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_RESIDENT) rotate_kernel(const
                     q = fma2(p, s, mul2(q, c));
                     p = x;
                 };
-                if (interleaved) {
+                if (IL) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (turns[k]) turn(lo[k], hi[k], c[k], s[k], ns[k]);
+                        if (turns[k]) turn(v[2 * k], v[2 * k + 1], c[k], s[k], ns[k]);
                 } else if (turns[0]) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        turn(lo[k], lo[k + 2], c[k], s[k], ns[k]);
-                        turn(hi[k], hi[k + 2], c[k + 2], s[k + 2], ns[k + 2]);
-                    }
+                    for (int k = 0; k < 4; ++k) turn(v[k], v[k + 4], c[k], s[k], ns[k]);
                 }
                 if (live) {
                     T* y = (w ? yr[1] : yr[0]) + h * dim;
 #pragma unroll
-                    for (int k = 0; k < PIECES; ++k) Piece<T>::store(y + at[k], lo + k * WORDS, hi + k * WORDS);
+                    for (int k = 0; k < PIECES; ++k) Piece<T, IL>::store(y + at[k], v + k * PE / 2);
                 }
             }
         }
@@ -261,7 +267,8 @@ cudaError_t rotate_launch(const Launch& L, RotArgs& a, int n_sms) {
     const long long blocks = ((long long)a.rows * a.parts + ROT_WARPS - 1) / ROT_WARPS;
     const int grid = (int)std::min<long long>(blocks, (long long)ROT_RESIDENT * n_sms);
     ProfScope ps(L, KC_LAYERNORM);
-    const cudaError_t e = launch_overlapped(L, rotate_kernel<T, NORM, LP>, grid, ROT_THREADS, 0, 1, a);
+    const cudaError_t e = a.table.interleaved && a.positions ? launch_overlapped(L, rotate_kernel<T, NORM, LP, true>, grid, ROT_THREADS, 0, 1, a)
+                                                             : launch_overlapped(L, rotate_kernel<T, NORM, LP, false>, grid, ROT_THREADS, 0, 1, a);
     BUMP(L);
     return e;
 }
