@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -476,39 +477,65 @@ def intra_coherence(contexts, co_norm):
 
 
 # ---- encoders that pack sequences of different lengths ----------------------------------------------
-def _here(where, dtype_name, *tensors):
-    """Refuses tensors of another element type, on the host or on another device than the current one."""
-    import torch
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for name, t, want in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda or t.get_device() != here:
-            raise PolymorphError(PM_ERR_ARG, where, f"{name} is not on the current device")
-        if t.dtype != (getattr(torch, dtype_name) if want is None else getattr(torch, want)):
-            raise PolymorphError(PM_ERR_ARG, where, f"{name} has type {t.dtype}")
+# A call's checks and marshalling cost more than a small kernel, so they look at each tensor once and fill the argument
+# struct with one pack.
+_types = None                  # element types by dtype
+_int32 = _float32 = None
+_device = None                 # () -> current device ordinal
+
+
+def _start():
+    """(current device, element types): torch is looked up once."""
+    global _types, _int32, _float32, _device
+    if _types is None:
+        import torch
+        _types = {0: torch.bfloat16, 1: torch.float32}
+        _int32, _float32 = torch.int32, torch.float32
+    if _device is None:
+        import torch
+        if not torch.cuda.is_available():
+            return None, _types
+        torch.cuda.current_stream()                        # initialises CUDA
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device(), _types
+
+
+def _refuse(where, detail):
+    raise PolymorphError(PM_ERR_ARG, where, detail)
+
+
+def _on(where, name, t, here, dtype):
+    """Refuses a tensor of another element type, on the host or on another device than the current one."""
+    if t.get_device() != here or here is None:
+        _refuse(where, f"{name} is not on the current device")
+    if t.dtype is not dtype:
+        _refuse(where, f"{name} has type {t.dtype}")
 
 
 def _heads(where, name, t):
     """(rows, heads, head_dim, elements between rows) of [rows, heads, head_dim] whose heads lie side by side in a row."""
-    if t.dim() != 3:
-        raise PolymorphError(PM_ERR_ARG, where, f"{name} is not [rows, heads, head_dim]")
-    (rows, heads, dim), (row, head, element) = t.shape, t.stride()
-    if (dim > 1 and element != 1) or (heads > 1 and head != dim):
-        raise PolymorphError(PM_ERR_ARG, where, f"the heads of a row of {name} do not lie side by side")
+    shape = t.shape
+    if len(shape) != 3:
+        _refuse(where, f"{name} is not [rows, heads, head_dim]")
+    (rows, heads, dim), (row, head, element) = shape, t.stride()
+    if (element != 1 and dim > 1) or (head != dim and heads > 1):
+        _refuse(where, f"the heads of a row of {name} do not lie side by side")
     return rows, heads, dim, row if rows > 1 else max(row, heads * dim)
 
 
-def _ints_of(where, name, t, *shapes):
-    """Refuses an index tensor that is not contiguous or has none of the shapes."""
-    if not t.is_contiguous() or tuple(t.shape) not in shapes:
-        raise PolymorphError(PM_ERR_ARG, where, f"{name} has shape {tuple(t.shape)} or is not contiguous")
+def _indexes(where, name, t, here, *lengths):
+    """Refuses an int32 index tensor that is not contiguous, on the current device and one of the lengths long; its address."""
+    _on(where, name, t, here, _int32)
+    if not t.is_contiguous() or t.numel() not in lengths:
+        _refuse(where, f"{name} has shape {tuple(t.shape)} or is not contiguous")
+    return t.data_ptr()
 
 
-def _type_name(where, dtype):
-    if dtype not in (0, 1):
-        raise PolymorphError(PM_ERR_ARG, where, "dtype is 0 (bf16) or 1 (fp32)")
-    return "bfloat16" if dtype == 0 else "float32"
+def _element_type(where, types, dtype):
+    t = types.get(dtype)
+    if t is None:
+        _refuse(where, "dtype is 0 (bf16) or 1 (fp32)")
+    return t
 
 
 class RopeTable:
@@ -527,55 +554,78 @@ class RopeTable:
         self.head_dim, self.axes, self.address = head_dim, axes, C.addressof(self.table)
 
 
-def _positions(where, positions, rows, axes):
-    _ints_of(where, "positions", positions, *([(rows,), (rows, 1)] if axes == 1 else [(rows, axes)]))
+def _positions(where, positions, rows, axes, here):
+    if positions.dim() != axes and not (axes == 1 and positions.dim() == 2 and positions.shape[1] == 1):
+        _refuse(where, f"positions has shape {tuple(positions.shape)}")
+    if positions.shape[0] != rows or (axes == 2 and positions.shape[1] != 2):
+        _refuse(where, f"positions has shape {tuple(positions.shape)}")
+    return _indexes(where, "positions", positions, here, rows * axes)
 
 
 def rope(x, y, positions, table, dtype, stream=None):
     """pm_rope: x, y = torch CUDA [rows, heads, head_dim] (y may be x), positions = torch CUDA int32 [rows] or [rows, 2]."""
-    lib, where = load(), "pm_rope"
-    name = _type_name(where, dtype)
-    _here(where, name, ("x", x, None), ("y", y, None), ("positions", positions, "int32"))
+    lib, where, (here, types) = load(), "pm_rope", _start()
+    t = _element_type(where, types, dtype)
+    _on(where, "x", x, here, t)
+    _on(where, "y", y, here, t)
     rows, heads, dim, xs = _heads(where, "x", x)
-    ys = _heads(where, "y", y)[3]
-    if y.shape != x.shape or dim != table.head_dim:
-        raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
-    _positions(where, positions, rows, table.axes)
-    rc = lib.pm_rope(_ptr(x), xs, _ptr(y), ys, _ptr(positions), rows, heads, table.address, dtype, _stream_ptr(stream))
+    shape = _heads(where, "y", y)
+    if shape[:3] != (rows, heads, dim) or dim != table.head_dim:
+        _refuse(where, "shapes differ")
+    at = _positions(where, positions, rows, table.axes, here)
+    rc = lib.pm_rope(x.data_ptr(), xs, y.data_ptr(), shape[3], at, rows, heads, table.address, dtype, _stream_ptr(stream))
     if rc != PM_OK:
         raise PolymorphError(rc, where)
+
+
+_NORM_ARGS = struct.Struct("@4P4q6P6ifi")                  # pm_qk_norm_rope_args
+_ATTENTION_ARGS = struct.Struct("@4P4q3P9ifiPPN")          # pm_packed_attention
+assert _NORM_ARGS.size == C.sizeof(pm_qk_norm_rope_args) and _ATTENTION_ARGS.size == C.sizeof(pm_packed_attention)
+
+
+def _weights(where, name, t, here, heads, dim, per_head):
+    """Address of fp32 weights [head_dim], or [heads, head_dim]; 0 for none."""
+    if t is None:
+        return 0
+    _on(where, name, t, here, _float32)
+    if not t.is_contiguous() or tuple(t.shape) != ((heads, dim) if per_head else (dim,)):
+        _refuse(where, f"{name} has shape {tuple(t.shape)} or is not contiguous")
+    return t.data_ptr()
 
 
 def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_beta=None, k_beta=None, positions=None, table=None, stream=None):
     """pm_qk_norm_rope: q, k and their outputs = torch CUDA [rows, heads, head_dim] (an output may be its input; k may be None);
     gamma, beta = torch CUDA fp32 [head_dim], or [heads, head_dim] for weights of each head; norm "rms" or "layer"."""
-    lib, where = load(), "pm_qk_norm_rope"
-    name = _type_name(where, dtype)
-    if norm not in NORMS:
-        raise PolymorphError(PM_ERR_ARG, where, "norm is rms or layer")
+    lib, where, (here, types) = load(), "pm_qk_norm_rope", _start()
+    t = _element_type(where, types, dtype)
+    kind = NORMS.get(norm)
+    if kind is None:
+        _refuse(where, "norm is rms or layer")
     if (table is None) != (positions is None):
-        raise PolymorphError(PM_ERR_ARG, where, "positions and table go together")
-    _here(where, name, ("q", q, None), ("k", k, None), ("q_out", q_out, None), ("k_out", k_out, None), ("positions", positions, "int32"),
-          *((n, t, "float32") for n, t in (("q_gamma", q_gamma), ("k_gamma", k_gamma), ("q_beta", q_beta), ("k_beta", k_beta))))
+        _refuse(where, "positions and table go together")
+    _on(where, "q", q, here, t)
+    _on(where, "q_out", q_out, here, t)
     rows, heads, dim, qs = _heads(where, "q", q)
-    qos = _heads(where, "q_out", q_out)[3]
-    kv_heads = ks = kos = 0
-    if k is not None:
-        _, kv_heads, _, ks = _heads(where, "k", k)
-        kos = _heads(where, "k_out", k_out)[3]
-        if k.shape != (rows, kv_heads, dim) or k_out.shape != k.shape:
-            raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
-    if q_out.shape != q.shape or (table is not None and dim != table.head_dim):
-        raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
+    q_shape = _heads(where, "q_out", q_out)
     per_head = q_gamma.dim() == 2
-    for n, t, h in (("q_gamma", q_gamma, heads), ("q_beta", q_beta, heads), ("k_gamma", k_gamma, kv_heads), ("k_beta", k_beta, kv_heads)):
-        if t is not None:
-            _ints_of(where, n, t, (h, dim) if per_head else (dim,))
-    if table is not None:
-        _positions(where, positions, rows, table.axes)
-    args = pm_qk_norm_rope_args(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), qs, ks, qos, kos, _ptr(q_gamma), _ptr(k_gamma), _ptr(q_beta), _ptr(k_beta),
-                                _ptr(positions), None if table is None else table.address, rows, heads, kv_heads, dim, NORMS[norm], int(per_head), eps, dtype)
-    rc = lib.pm_qk_norm_rope(C.byref(args), _stream_ptr(stream))
+    kv_heads = ks = kos = kp = kop = 0
+    if k is not None:
+        _on(where, "k", k, here, t)
+        _on(where, "k_out", k_out, here, t)
+        k_rows, kv_heads, k_dim, ks = _heads(where, "k", k)
+        k_shape = _heads(where, "k_out", k_out)
+        if (k_rows, k_dim) != (rows, dim) or k_shape[:3] != (rows, kv_heads, dim):
+            _refuse(where, "shapes differ")
+        kos, kp, kop = k_shape[3], k.data_ptr(), k_out.data_ptr()
+    if q_shape[:3] != (rows, heads, dim) or (table is not None and dim != table.head_dim):
+        _refuse(where, "shapes differ")
+    args = _NORM_ARGS.pack(
+        q.data_ptr(), kp, q_out.data_ptr(), kop, qs, ks, q_shape[3], kos,
+        _weights(where, "q_gamma", q_gamma, here, heads, dim, per_head), _weights(where, "k_gamma", k_gamma, here, kv_heads, dim, per_head),
+        _weights(where, "q_beta", q_beta, here, heads, dim, per_head), _weights(where, "k_beta", k_beta, here, kv_heads, dim, per_head),
+        0 if table is None else _positions(where, positions, rows, table.axes, here), 0 if table is None else table.address,
+        rows, heads, kv_heads, dim, kind, per_head, eps, dtype)
+    rc = lib.pm_qk_norm_rope(args, _stream_ptr(stream))
     if rc != PM_OK:
         raise PolymorphError(rc, where)
 
@@ -583,44 +633,57 @@ def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_be
 LONG_HISTORY = 4096            # keys below which no call has a use for a workspace
 
 
-def _lend_workspace(lib, args, like, stream):
-    """Memory of torch's for the time of the call on its stream."""
+def _workspace(lib, args, like, stream):
+    """Memory of torch's for the time of the call on its stream, or None."""
     import torch
     need = C.c_size_t(0)
     sms = torch.cuda.get_device_properties(like.device).multi_processor_count
-    rc = lib.pm_attention_packed_workspace(C.byref(args), sms, C.byref(need))
+    rc = lib.pm_attention_packed_workspace(args, sms, C.byref(need))
     if rc != PM_OK:
         raise PolymorphError(rc, "pm_attention_packed_workspace")
-    if need.value:
-        space = torch.empty(need.value, dtype=torch.uint8, device=like.device)
-        if stream is not None:
-            space.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream)))
-        args.workspace, args.workspace_bytes = space.data_ptr(), need.value
+    if not need.value:
+        return None
+    space = torch.empty(need.value, dtype=torch.uint8, device=like.device)
+    if stream is not None:
+        space.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream)))
+    return space
 
 
 def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offsets=None, kv_lengths=None, causal=False, scale=None, status=None,
                      stream=None):
     """pm_attention_packed: q, out = torch CUDA [rows, heads, head_dim], k, v = [kv rows, kv_heads, head_dim]; q_offsets = torch CUDA int32
     [n + 1]; kv_offsets = the same for keys ([n] suffices with kv_lengths = [n]); status = torch CUDA int32 [1] or None."""
-    lib, where = load(), "pm_attention_packed"
-    name = _type_name(where, dtype)
-    _here(where, name, ("q", q, None), ("k", k, None), ("v", v, None), ("out", out, None),
-          *((n, t, "int32") for n, t in (("q_offsets", q_offsets), ("kv_offsets", kv_offsets), ("kv_lengths", kv_lengths), ("status", status))))
+    lib, where, (here, types) = load(), "pm_attention_packed", _start()
+    t = _element_type(where, types, dtype)
+    _on(where, "q", q, here, t)
+    _on(where, "k", k, here, t)
+    _on(where, "v", v, here, t)
+    _on(where, "out", out, here, t)
     rows, heads, dim, qs = _heads(where, "q", q)
-    kv_rows, kv_heads, _, ks = _heads(where, "k", k)
-    vs, os_ = _heads(where, "v", v)[3], _heads(where, "out", out)[3]
-    if k.shape != v.shape or out.shape != q.shape or k.shape[2] != dim:
-        raise PolymorphError(PM_ERR_ARG, where, "shapes differ")
+    kv_rows, kv_heads, k_dim, ks = _heads(where, "k", k)
+    v_shape, o_shape = _heads(where, "v", v), _heads(where, "out", out)
+    if k_dim != dim or v_shape[:3] != (kv_rows, kv_heads, dim) or o_shape[:3] != (rows, heads, dim):
+        _refuse(where, "shapes differ")
+    if scale is not None and not scale > 0:
+        _refuse(where, "scale is positive")
     n = q_offsets.numel() - 1
-    _ints_of(where, "q_offsets", q_offsets, (n + 1,))
-    if kv_offsets is not None:
-        _ints_of(where, "kv_offsets", kv_offsets, (n + 1,), *([(n,)] if kv_lengths is not None else []))
+    qo, ko, kl, sp = _indexes(where, "q_offsets", q_offsets, here, n + 1), 0, 0, 0
     if kv_lengths is not None:
-        _ints_of(where, "kv_lengths", kv_lengths, (n,))
-    args = pm_packed_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(out), qs, ks, vs, os_, _ptr(q_offsets), _ptr(kv_offsets), _ptr(kv_lengths), rows, kv_rows, n,
-                               int(max_q), int(max_kv), heads, kv_heads, dim, int(bool(causal)), 0.0 if scale is None else scale, dtype, _ptr(status))
-    if dtype == 0 and max_kv >= LONG_HISTORY and max_q * heads <= 64 * kv_heads:
-        _lend_workspace(lib, args, q, stream)
-    rc = lib.pm_attention_packed(C.byref(args), _stream_ptr(stream))
+        kl = _indexes(where, "kv_lengths", kv_lengths, here, n)
+        if kv_offsets is None:
+            _refuse(where, "kv_lengths without kv_offsets")
+        ko = _indexes(where, "kv_offsets", kv_offsets, here, n, n + 1)
+    elif kv_offsets is not None:
+        ko = _indexes(where, "kv_offsets", kv_offsets, here, n + 1)
+    if status is not None:
+        sp = _indexes(where, "status", status, here, 1)
+    fields = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), qs, ks, v_shape[3], o_shape[3], qo, ko, kl, rows, kv_rows, n, max_q, max_kv, heads,
+              kv_heads, dim, 1 if causal else 0, 0.0 if scale is None else scale, dtype, sp)
+    args = _ATTENTION_ARGS.pack(*fields, 0, 0)
+    if max_kv >= LONG_HISTORY and dtype == 0 and max_q * heads <= 64 * kv_heads:
+        space = _workspace(lib, args, q, stream)
+        if space is not None:
+            args = _ATTENTION_ARGS.pack(*fields, space.data_ptr(), space.numel())
+    rc = lib.pm_attention_packed(args, _stream_ptr(stream))
     if rc != PM_OK:
         raise PolymorphError(rc, where)
