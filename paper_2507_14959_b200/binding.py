@@ -555,9 +555,7 @@ class RopeTable:
 
 
 def _positions(where, positions, rows, axes, here):
-    if positions.dim() != axes and not (axes == 1 and positions.dim() == 2 and positions.shape[1] == 1):
-        _refuse(where, f"positions has shape {tuple(positions.shape)}")
-    if positions.shape[0] != rows or (axes == 2 and positions.shape[1] != 2):
+    if positions.shape != ((rows,) if axes == 1 else (rows, 2)) and positions.shape != (rows, axes):
         _refuse(where, f"positions has shape {tuple(positions.shape)}")
     return _indexes(where, "positions", positions, here, rows * axes)
 
@@ -588,7 +586,7 @@ def _weights(where, name, t, here, heads, dim, per_head):
     if t is None:
         return 0
     _on(where, name, t, here, _float32)
-    if not t.is_contiguous() or tuple(t.shape) != ((heads, dim) if per_head else (dim,)):
+    if t.shape != ((heads, dim) if per_head else (dim,)) or not t.is_contiguous():
         _refuse(where, f"{name} has shape {tuple(t.shape)} or is not contiguous")
     return t.data_ptr()
 

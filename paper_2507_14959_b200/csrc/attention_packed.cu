@@ -12,6 +12,7 @@
 
 #include <algorithm>
 
+#include "f32x2.cuh"
 #include "packed.cuh"
 
 #define BUMP(L) do { if ((L).launches) ++*(L).launches; } while (0)
@@ -353,7 +354,8 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) attention_join_kernel(const _
 // ---------------------------------------------------------------------------------------
 // fp32 on CUDA cores: R rows (64, or 16 where there are few) per CTA, keys 64 at a time.  256 threads as 16 x 16: thread (ty, tx) forms
 // the scores of rows ty + 16 i and keys tx + 16 j and the output of its rows at columns 4 tx + 64 j.  Rows of Q and K lie D + 4 floats
-// apart, so that the 16-byte reads of eight neighbouring threads touch all banks once; P takes the place of K.
+// apart, so that the 16-byte reads of eight neighbouring threads touch all banks once; P takes the place of K.  Products run packed, two
+// results per instruction: one at a time the floating-point unit gives half its rate.
 // ---------------------------------------------------------------------------------------
 constexpr int F32_KEYS = 64;
 template <int D, int R>
@@ -365,7 +367,7 @@ struct F32Smem {
 };
 
 template <int D, int R>
-__global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constant__ PackedArgs a, int cluster) {
+__global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_constant__ PackedArgs a, int cluster) {
     constexpr int RT = R / 16, DT = D / 64;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     F32Smem<D, R>& sm = *reinterpret_cast<F32Smem<D, R>*>(smem_raw);
@@ -388,13 +390,14 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
         *reinterpret_cast<float4*>(&sm.q[r][c]) = x;
     }
     int vis[RT];
-    float m[RT], l[RT], o[RT][DT][4];
+    float m[RT], l[RT];
+    uint64_t o[RT][DT][2];                                              // four columns, packed
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         vis[i] = packed_visible(seg, min(r0 + ty + 16 * i, rows - 1) / a.group, a.causal);
         m[i] = -INFINITY; l[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < DT; ++j) o[i][j][0] = o[i][j][1] = o[i][j][2] = o[i][j][3] = 0.f;
+        for (int j = 0; j < DT; ++j) o[i][j][0] = o[i][j][1] = 0ull;
     }
     // a warp (two thread rows) without a real row in it only helps to copy; the warp as a whole, for its shuffles
     const bool active = R > 16 || r0 + (ty & ~1) < rows;
@@ -413,24 +416,30 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
         copy_wait<0>();
         __syncthreads();
         float s[RT][4];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
         if (active) {
+            uint64_t s2[RT][4];                                         // sums of the even and of the odd dimensions
+#pragma unroll
+            for (int i = 0; i < RT; ++i) s2[i][0] = s2[i][1] = s2[i][2] = s2[i][3] = 0ull;
 #pragma unroll 4
             for (int d = 0; d < D; d += 4) {
-                float4 q[RT], k[4];
+                ulonglong2 q[RT], k[4];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) q[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][d]);
+                for (int i = 0; i < RT; ++i) q[i] = *reinterpret_cast<const ulonglong2*>(&sm.q[ty + 16 * i][d]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
+                for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const ulonglong2*>(&sm.k[tx + 16 * j][d]);
 #pragma unroll
                 for (int i = 0; i < RT; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[i][j] = fmaf(q[i].x, k[j].x, s[i][j]); s[i][j] = fmaf(q[i].y, k[j].y, s[i][j]);
-                        s[i][j] = fmaf(q[i].z, k[j].z, s[i][j]); s[i][j] = fmaf(q[i].w, k[j].w, s[i][j]);
-                    }
+                    for (int j = 0; j < 4; ++j) s2[i][j] = fma2(q[i].y, k[j].y, fma2(q[i].x, k[j].x, s2[i][j]));
             }
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float a0, a1;
+                    upk2(s2[i][j], a0, a1);
+                    s[i][j] = a0 + a1;
+                }
         }
         __syncthreads();                                                // P goes where the keys were
         if (active) {
@@ -454,7 +463,7 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
                     ps[ty + 16 * i][tx + 16 * j] = p;
                 }
 #pragma unroll
-                for (int j = 0; j < DT; ++j) { o[i][j][0] *= f; o[i][j][1] *= f; o[i][j][2] *= f; o[i][j][3] *= f; }
+                for (int j = 0; j < DT; ++j) { o[i][j][0] = mul2(o[i][j][0], pk2(f, f)); o[i][j][1] = mul2(o[i][j][1], pk2(f, f)); }
             }
         }
         __syncthreads();
@@ -465,17 +474,23 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
 #pragma unroll
                 for (int i = 0; i < RT; ++i) p[i] = *reinterpret_cast<const float4*>(&ps[ty + 16 * i][t]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) {
+                    uint64_t w[RT];
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        const float x = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
+                        w[i] = pk2(x, x);
+                    }
 #pragma unroll
                     for (int j = 0; j < DT; ++j) {
-                        const float4 v = *reinterpret_cast<const float4*>(&sm.v[t + e][4 * tx + 64 * j]);
+                        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&sm.v[t + e][4 * tx + 64 * j]);
 #pragma unroll
                         for (int i = 0; i < RT; ++i) {
-                            const float w = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
-                            o[i][j][0] = fmaf(w, v.x, o[i][j][0]); o[i][j][1] = fmaf(w, v.y, o[i][j][1]);
-                            o[i][j][2] = fmaf(w, v.z, o[i][j][2]); o[i][j][3] = fmaf(w, v.w, o[i][j][3]);
+                            o[i][j][0] = fma2(w[i], v.x, o[i][j][0]);
+                            o[i][j][1] = fma2(w[i], v.y, o[i][j][1]);
                         }
                     }
+                }
             }
         }
     }
@@ -494,7 +509,7 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
             if (row < rows)
 #pragma unroll
                 for (int j = 0; j < DT; ++j)
-                    *reinterpret_cast<float4*>(address(row, 4 * tx + 64 * j)) = make_float4(o[i][j][0] * inv, o[i][j][1] * inv, o[i][j][2] * inv, o[i][j][3] * inv);
+                    *reinterpret_cast<ulonglong2*>(address(row, 4 * tx + 64 * j)) = make_ulonglong2(mul2(o[i][j][0], pk2(inv, inv)), mul2(o[i][j][1], pk2(inv, inv)));
         }
         return;
     }
@@ -503,7 +518,7 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
 #pragma unroll
-        for (int j = 0; j < DT; ++j) *reinterpret_cast<float4*>(&sm.q[ty + 16 * i][4 * tx + 64 * j]) = make_float4(o[i][j][0], o[i][j][1], o[i][j][2], o[i][j][3]);
+        for (int j = 0; j < DT; ++j) *reinterpret_cast<ulonglong2*>(&sm.q[ty + 16 * i][4 * tx + 64 * j]) = make_ulonglong2(o[i][j][0], o[i][j][1]);
         if (tx == 0) { sm.m[ty + 16 * i] = m[i]; sm.l[ty + 16 * i] = l[i]; }
     }
     cluster_sync_all();
@@ -529,13 +544,13 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const __grid_constan
 }
 
 // CTAs that share the keys of a row tile: while the grid leaves room for them and each still has `least` keys; and of long histories, whose
-// lengths may differ, up to eight times as many CTAs as run at once, each with ROWS_EVEN_KEYS still, so that they end together (48 streams of
+// lengths may differ, up to eight times as many CTAs as run at once, each with `even` keys still, so that they end together (48 streams of
 // up to 8192 keys: 133 us with a CTA each, 126 with two, 118 with four)
-constexpr int ROWS_EVEN_KEYS = 512;
-int key_split(long long ctas, long long slots, int max_kv, int least) {
+constexpr int ROWS_EVEN_KEYS = 512, F32_EVEN_KEYS = 256;
+int key_split(long long ctas, long long slots, int max_kv, int least, int even) {
     int c = 1;
     while (c < ROWS_MAX_CLUSTER && ((ctas * c * 2 <= slots && (long long)max_kv >= 2ll * c * least) ||
-                                    (ctas * c * 2 <= 8 * slots && (long long)max_kv >= 2ll * c * ROWS_EVEN_KEYS)))
+                                    (ctas * c * 2 <= 8 * slots && (long long)max_kv >= 2ll * c * even)))
         c *= 2;
     return c;
 }
@@ -546,7 +561,7 @@ struct RowsForm { int tiles, cluster, splits; };
 RowsForm rows_form(const PackedArgs& a, int n_sms) {
     const int tiles = (int)(((long long)a.max_q * a.group + 15) / 16);
     const long long ctas = (long long)tiles * a.kv_heads * a.n_seqs, slots = 2ll * n_sms;
-    RowsForm f = {tiles, key_split(ctas, slots, a.max_kv, 16 * ROWS_WARPS), 1};
+    RowsForm f = {tiles, key_split(ctas, slots, a.max_kv, 16 * ROWS_WARPS, ROWS_EVEN_KEYS), 1};
     if (f.cluster == ROWS_MAX_CLUSTER && ctas * f.cluster * 2 <= slots) {
         const long long splits = std::min(slots / ctas, (long long)a.max_kv / (ROWS_SPLIT_KEYS * ROWS_WARPS));
         if (splits >= 2 * ROWS_MAX_CLUSTER) f.splits = (int)splits;
@@ -579,7 +594,7 @@ cudaError_t launch_rows(const Launch& L, const PackedArgs& a, int n_sms, void* w
 template <int D, int R>
 cudaError_t launch_f32(const Launch& L, const PackedArgs& a, int n_sms) {
     const int tiles = (int)(((long long)a.max_q * a.group + R - 1) / R);
-    const int cluster = key_split((long long)tiles * a.kv_heads * a.n_seqs, 2ll * n_sms, a.max_kv, F32_KEYS);
+    const int cluster = key_split((long long)tiles * a.kv_heads * a.n_seqs, 2ll * n_sms, a.max_kv, F32_KEYS, F32_EVEN_KEYS);
     static SmemGrant grant;
     if (cudaError_t e = grant.ensure(attention_f32_kernel<D, R>, (int)sizeof(F32Smem<D, R>)); e != cudaSuccess) return e;
     ProfScope ps(L, KC_ATTENTION);
