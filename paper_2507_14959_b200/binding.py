@@ -25,7 +25,7 @@ EXPORTS = [
     "pm_select_static", "pm_metrics_reset", "pm_metrics_read", "pm_status", "pm_last_error", "pm_launch_count", "pm_set_graphs", "pm_set_small_batch_kernel", "pm_profile_enable", "pm_profile_read", "pm_plan_stats", "pm_linear_create", "pm_linear_register",
     "pm_linear_forward", "pm_linear_status", "pm_linear_last_error", "pm_linear_destroy",
     "pm_layernorm", "pm_attention", "pm_selftest_wait_timeout", "pm_linear_kernel", "pm_cooccurrence", "pm_build_contexts", "pm_intra_coherence",
-    "pm_rope_init", "pm_rope", "pm_qk_norm_rope", "pm_attention_packed", "pm_attention_packed_workspace",
+    "pm_rope_init", "pm_rope", "pm_qk_norm_rope", "pm_attention_packed", "pm_attention_packed_workspace", "pm_attention_packed_kernel",
 ]
 
 
@@ -145,6 +145,7 @@ def load():
     lib.pm_qk_norm_rope.argtypes = [vp, vp]
     lib.pm_attention_packed.argtypes = [vp, vp]
     lib.pm_attention_packed_workspace.argtypes = [vp, ip, C.POINTER(C.c_size_t)]
+    lib.pm_attention_packed_kernel.argtypes = [vp, ip, C.POINTER(C.c_int32)]
     _lib = lib
     return lib
 
@@ -628,7 +629,8 @@ def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_be
         raise PolymorphError(rc, where)
 
 
-LONG_HISTORY = 4096            # keys below which no call has a use for a workspace
+LONG_HISTORY = 4096            # keys below which, and tiles of 16 rows above which, no call has a use for a workspace
+FEW_TILES = 32
 
 
 def _workspace(lib, args, like, stream):
@@ -678,10 +680,23 @@ def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offset
     fields = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), qs, ks, v_shape[3], o_shape[3], qo, ko, kl, rows, kv_rows, n, max_q, max_kv, heads,
               kv_heads, dim, 1 if causal else 0, 0.0 if scale is None else scale, dtype, sp)
     args = _ATTENTION_ARGS.pack(*fields, 0, 0)
-    if max_kv >= LONG_HISTORY and dtype == 0 and max_q * heads <= 64 * kv_heads:
+    if max_kv >= LONG_HISTORY and dtype == 0 and n * kv_heads * ((max_q * (heads // kv_heads) + 15) // 16) <= FEW_TILES:
         space = _workspace(lib, args, q, stream)
         if space is not None:
             args = _ATTENTION_ARGS.pack(*fields, space.data_ptr(), space.numel())
     rc = lib.pm_attention_packed(args, _stream_ptr(stream))
     if rc != PM_OK:
         raise PolymorphError(rc, where)
+
+
+def attention_packed_kernel(*, heads, kv_heads, head_dim, n_seqs, max_q, max_kv, q_rows=None, kv_rows=None, dtype=0, workspace_bytes=0, n_sms=148):
+    """pm_attention_packed_kernel for a call of these sizes: ("16 rows", "tcgen05" or "fp32", CTAs of a cluster, CTAs through the workspace)."""
+    q_rows, kv_rows = n_seqs * max_q if q_rows is None else q_rows, n_seqs * max_kv if kv_rows is None else kv_rows
+    some = 1 << 20                                         # an aligned address; nothing is read
+    args = _ATTENTION_ARGS.pack(some, some, some, some, heads * head_dim, kv_heads * head_dim, kv_heads * head_dim, heads * head_dim, some, some, 0, q_rows,
+                                kv_rows, n_seqs, max_q, max_kv, heads, kv_heads, head_dim, 1, 0.0, dtype, 0, some if workspace_bytes else 0, workspace_bytes)
+    form = (C.c_int32 * 3)()
+    rc = load().pm_attention_packed_kernel(args, n_sms, form)
+    if rc != PM_OK:
+        raise PolymorphError(rc, "pm_attention_packed_kernel")
+    return ("16 rows", "tcgen05", "fp32", "none")[form[0]], form[1], form[2]

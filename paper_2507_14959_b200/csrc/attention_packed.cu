@@ -71,6 +71,7 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
 constexpr int ROWS_WARPS = 4;
 constexpr int ROWS_STAGES = 3;
 constexpr int ROWS_MAX_CLUSTER = 8;
+constexpr int PACKED_TC_ROWS = 256;          // rows of a unit of the tcgen05 kernel
 constexpr int ROWS_SPLIT_KEYS = 64;          // keys of a warp below which a split is not worth its part
 
 template <int D>
@@ -558,15 +559,32 @@ int key_split(long long ctas, long long slots, int max_kv, int least, int even) 
 // How the keys of a row tile are shared: a cluster joins in shared memory, up to eight CTAs; where even those leave most of the GPU idle and
 // there is a workspace, any number of CTAs leave their parts there and a second kernel joins them.
 struct RowsForm { int tiles, cluster, splits; };
-RowsForm rows_form(const PackedArgs& a, int n_sms) {
+RowsForm rows_form(const PackedArgs& a, int n_sms, bool workspace) {
     const int tiles = (int)(((long long)a.max_q * a.group + 15) / 16);
     const long long ctas = (long long)tiles * a.kv_heads * a.n_seqs, slots = 2ll * n_sms;
     RowsForm f = {tiles, key_split(ctas, slots, a.max_kv, 16 * ROWS_WARPS, ROWS_EVEN_KEYS), 1};
-    if (f.cluster == ROWS_MAX_CLUSTER && ctas * f.cluster * 2 <= slots) {
+    if (workspace && f.cluster == ROWS_MAX_CLUSTER && ctas * f.cluster * 2 <= slots) {
         const long long splits = std::min(slots / ctas, (long long)a.max_kv / (ROWS_SPLIT_KEYS * ROWS_WARPS));
-        if (splits >= 2 * ROWS_MAX_CLUSTER) f.splits = (int)splits;
+        if (splits >= 2 * ROWS_MAX_CLUSTER) f = {tiles, 1, (int)splits};
     }
     return f;
+}
+// Whether 16-row tiles serve, by what both kernels take in us as measured on a B200 (twenty shapes of 1 to 256 sequences, 16 to 1024 rows per K/V
+// head and 17 to 16000 keys: within a third of either kernel's time, and the faster one is chosen in every one of them).
+//   16-row tiles:  3, joining 2 (4 through a workspace); a CTA 0.55 and per 16 keys 0.07 (head dim 64) or 0.15 (128) beside another on its
+//                  multiprocessor, 1.6 times that alone
+//   tcgen05:       5; a unit of 256 rows 1.3 and per block of 64 keys 0.76, whatever its rows: two tiles' chains of dependent steps
+// Lengths are the call's limits, or what the buffers hold per sequence.
+bool few_rows(const PackedArgs& a, int head_dim, const RowsForm& f, int n_sms) {
+    if (a.kv_rows == 0) return true;
+    const double seqs = a.n_seqs, rows = std::min(seqs * a.max_q, (double)a.q_rows) * a.group, keys = std::min((double)a.max_kv, a.kv_rows / seqs);
+    const double share = (double)f.cluster * f.splits, ctas = std::min(seqs * f.tiles, rows / 16 + seqs) * a.kv_heads * share;
+    const double per_16 = (head_dim == 64 ? 0.07 : 0.15) * (ctas < n_sms ? 1.6 : 1.0);
+    const double t_rows = 3.0 + (f.splits > 1 ? 4.0 : f.cluster > 1 ? 2.0 : 0.0) + std::max(ctas / n_sms, 1.0) * (0.55 + per_16 * keys / (16.0 * share));
+    const double per_unit = PACKED_TC_ROWS / a.group * a.group;
+    const double units = std::min(seqs * ceil((double)a.max_q * a.group / per_unit), rows / per_unit + seqs) * a.kv_heads;
+    const double t_tc = 5.0 + ceil(units / n_sms) * (1.3 + 0.76 * ceil(keys / 64.0));
+    return t_rows < t_tc;
 }
 size_t rows_workspace(const PackedArgs& a, int head_dim, const RowsForm& f) {
     if (f.splits == 1) return 0;
@@ -574,10 +592,7 @@ size_t rows_workspace(const PackedArgs& a, int head_dim, const RowsForm& f) {
 }
 
 template <int D>
-cudaError_t launch_rows(const Launch& L, const PackedArgs& a, int n_sms, void* workspace, size_t bytes) {
-    RowsForm f = rows_form(a, n_sms);
-    if (!workspace || bytes < rows_workspace(a, D, f)) f.splits = 1;
-    if (f.splits > 1) f.cluster = 1;
+cudaError_t launch_rows(const Launch& L, const PackedArgs& a, const RowsForm& f, void* workspace) {
     RowsPart<D>* parts = (RowsPart<D>*)workspace;
     static SmemGrant grant;
     if (cudaError_t e = grant.ensure(attention_rows_kernel<D>, (int)sizeof(RowsSmem<D>)); e != cudaSuccess) return e;
@@ -591,19 +606,23 @@ cudaError_t launch_rows(const Launch& L, const PackedArgs& a, int n_sms, void* w
     BUMP(L);
     return e;
 }
+struct F32Form { int rows, tiles, cluster; };
+F32Form f32_form(const PackedArgs& a, int n_sms) {
+    const long long rows = (long long)a.max_q * a.group;
+    F32Form f = {rows <= 16 ? 16 : 64, 0, 1};
+    f.tiles = (int)((rows + f.rows - 1) / f.rows);
+    f.cluster = key_split((long long)f.tiles * a.kv_heads * a.n_seqs, 2ll * n_sms, a.max_kv, F32_KEYS, F32_EVEN_KEYS);
+    return f;
+}
 template <int D, int R>
-cudaError_t launch_f32(const Launch& L, const PackedArgs& a, int n_sms) {
-    const int tiles = (int)(((long long)a.max_q * a.group + R - 1) / R);
-    const int cluster = key_split((long long)tiles * a.kv_heads * a.n_seqs, 2ll * n_sms, a.max_kv, F32_KEYS, F32_EVEN_KEYS);
+cudaError_t launch_f32(const Launch& L, const PackedArgs& a, const F32Form& f) {
     static SmemGrant grant;
     if (cudaError_t e = grant.ensure(attention_f32_kernel<D, R>, (int)sizeof(F32Smem<D, R>)); e != cudaSuccess) return e;
     ProfScope ps(L, KC_ATTENTION);
-    cudaError_t e = launch_overlapped(L, attention_f32_kernel<D, R>, dim3(tiles * cluster, a.kv_heads, a.n_seqs), 256, sizeof(F32Smem<D, R>), cluster, a, cluster);
+    cudaError_t e = launch_overlapped(L, attention_f32_kernel<D, R>, dim3(f.tiles * f.cluster, a.kv_heads, a.n_seqs), 256, sizeof(F32Smem<D, R>), f.cluster, a, f.cluster);
     BUMP(L);
     return e;
 }
-
-constexpr int PACKED_FEW_ROWS = 64;          // rows of a (sequence, K/V head) pair up to which 16-row tiles serve
 
 bool heads_ok(const void* p, long long stride, int heads, int dim, int dtype) {
     return p && ((uintptr_t)p & 15) == 0 && stride >= (long long)heads * dim && stride % (dtype == 0 ? 8 : 4) == 0;
@@ -613,7 +632,12 @@ bool heads_ok(const void* p, long long stride, int heads, int dim, int dtype) {
 
 namespace {
 
-bool few_rows(const PackedArgs& a) { return a.kv_rows == 0 || (long long)a.max_q * a.group <= PACKED_FEW_ROWS; }
+// Whether 16-row tiles serve a bf16 call with the workspace it has, and their form.
+bool bf16_form(const pm_packed_attention* p, const PackedArgs& a, int n_sms, RowsForm& f) {
+    f = rows_form(a, n_sms, p->workspace != nullptr);
+    if (p->workspace_bytes < rows_workspace(a, p->head_dim, f)) f = rows_form(a, n_sms, false);
+    return few_rows(a, p->head_dim, f, n_sms);
+}
 
 // Checks everything the host can see; PM_OK with nothing to do leaves a.n_seqs 0.
 int packed_args(const pm_packed_attention* p, PackedArgs& a) {
@@ -649,7 +673,28 @@ int pm_attention_packed_workspace(const pm_packed_attention* p, int n_sms, size_
     PackedArgs a;
     if (!bytes || n_sms <= 0) return PM_ERR_ARG;
     if (const int rc = packed_args(p, a); rc != PM_OK) return rc;
-    *bytes = a.n_seqs > 0 && p->dtype == 0 && few_rows(a) ? rows_workspace(a, p->head_dim, rows_form(a, n_sms)) : 0;
+    *bytes = 0;
+    if (a.n_seqs > 0 && p->dtype == 0) {
+        const RowsForm f = rows_form(a, n_sms, true);
+        if (few_rows(a, p->head_dim, f, n_sms)) *bytes = rows_workspace(a, p->head_dim, f);
+    }
+    return PM_OK;
+}
+
+int pm_attention_packed_kernel(const pm_packed_attention* p, int n_sms, int32_t* form) {
+    PackedArgs a;
+    if (!form || n_sms <= 0) return PM_ERR_ARG;
+    if (const int rc = packed_args(p, a); rc != PM_OK) return rc;
+    form[0] = -1; form[1] = form[2] = 1;
+    if (a.n_seqs == 0) return PM_OK;
+    if (p->dtype == 1) {
+        const F32Form f = f32_form(a, n_sms);
+        form[0] = 2; form[1] = f.cluster;
+        return PM_OK;
+    }
+    RowsForm f;
+    form[0] = bf16_form(p, a, n_sms, f) ? 0 : 1;
+    if (form[0] == 0) { form[1] = f.cluster; form[2] = f.splits; }
     return PM_OK;
 }
 
@@ -672,12 +717,13 @@ int pm_attention_packed(const pm_packed_attention* p, void* cuda_stream) {
     L.st = st;
     L.status = a.status;
     cudaError_t e;
+    RowsForm f;
     if (p->dtype == 1) {
-        const bool few = (long long)a.max_q * a.group <= 16;
-        e = p->head_dim == 64 ? (few ? launch_f32<64, 16>(L, a, n_sms) : launch_f32<64, 64>(L, a, n_sms))
-                              : (few ? launch_f32<128, 16>(L, a, n_sms) : launch_f32<128, 64>(L, a, n_sms));
-    } else if (few_rows(a)) {
-        e = p->head_dim == 64 ? launch_rows<64>(L, a, n_sms, p->workspace, p->workspace_bytes) : launch_rows<128>(L, a, n_sms, p->workspace, p->workspace_bytes);
+        const F32Form f = f32_form(a, n_sms);
+        e = p->head_dim == 64 ? (f.rows == 16 ? launch_f32<64, 16>(L, a, f) : launch_f32<64, 64>(L, a, f))
+                              : (f.rows == 16 ? launch_f32<128, 16>(L, a, f) : launch_f32<128, 64>(L, a, f));
+    } else if (bf16_form(p, a, n_sms, f)) {
+        e = p->head_dim == 64 ? launch_rows<64>(L, a, f, p->workspace) : launch_rows<128>(L, a, f, p->workspace);
     } else {
         e = launch_packed_tc(L, a, p->head_dim, n_sms);
     }

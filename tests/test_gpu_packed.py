@@ -50,9 +50,10 @@ FILL = 7.0
 
 
 def check(dtype, dim, heads, kv_heads, lengths, causal=False, *, seed=0, packed=False, gap=0, slots=False, scale=None, pad=3, size=1.0, poison=True, call=None,
-          max_q=None, max_kv=None):
+          max_q=None, max_kv=None, kernel=None):
     """lengths: (queries, keys) of each sequence.  packed: q, k and v are ranges of one projection; gap: rows between sequences that belong
-    to none; slots: keys in slots of a cache with kv_lengths; poison: NaN in every row that belongs to no sequence."""
+    to none; slots: keys in slots of a cache with kv_lengths; poison: NaN in every row that belongs to no sequence; kernel: the one that the call has
+    to take."""
     from paper_2507_14959_b200 import binding
     t = TYPES[dtype]
     n_q, n_k = [a for a, _ in lengths], [b for _, b in lengths]
@@ -89,6 +90,13 @@ def check(dtype, dim, heads, kv_heads, lengths, causal=False, *, seed=0, packed=
     def run():
         binding.attention_packed(q, k, v, view, ints(q_at.tolist()), max(n_q) if max_q is None else max_q, max(n_k) if max_kv is None else max_kv, dtype, kv_offsets=kv_offsets,
                                  kv_lengths=kv_lengths, causal=causal, scale=scale, status=status)
+    if kernel:
+        need = 1 << 24 if kernel == "workspace" else 0
+        form = binding.attention_packed_kernel(heads=heads, kv_heads=kv_heads, head_dim=dim, n_seqs=len(lengths), max_q=max(n_q) if max_q is None else max_q,
+                                               max_kv=max(n_k) if max_kv is None else max_kv, q_rows=rows, kv_rows=len(k), dtype=dtype, workspace_bytes=need)
+        assert form[0] == ("16 rows" if kernel in ("cluster", "workspace") else kernel), form
+        assert kernel != "cluster" or form[1] > 1
+        assert kernel != "workspace" or form[2] > 1
     (call or (lambda f: f()))(run)
     torch.cuda.synchronize()
     assert status.item() == 0
@@ -150,6 +158,143 @@ def test_growing_scores(dim, causal):
     """Peaked rows whose maximum keeps rising: what has been summed is taken down again and again."""
     check(0, dim, 4, 4, [(300, 300), (700, 700)], causal, packed=True, size=3.0, seed=21)
     check(0, dim, 4, 2, [(1, 3000), (1, 64)], causal, size=30.0, seed=22)
+
+
+# Calls large enough for the tcgen05 kernel, whatever edges their sequences have.
+SHORT = [(n, n) for n in (1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 197, 255, 256, 257, 320)]
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_units_of_every_length(dim, causal):
+    check(0, dim, 8, 8, SHORT * 12, causal, packed=True, kernel="tcgen05", seed=31)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_units_without_keys_and_rows_that_see_nothing(dim, causal):
+    check(0, dim, 6, 6, [(0, 0), (5, 0), (0, 7), (9, 3), (1, 1), (130, 2), (300, 40), (2, 200), (400, 130), (256, 0), (130, 700), (0, 0)] * 14, causal, kernel="tcgen05",
+          seed=32)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(3, 1, 64), (5, 1, 128), (14, 2, 64), (48, 1, 128), (64, 1, 64), (32, 8, 128), (33, 3, 64)])
+def test_units_of_grouped_heads(heads, kv_heads, dim):
+    check(0, dim, heads, kv_heads, [(1 + i * 37 % 300, 1 + i * 37 % 300 + (i % 3) * 100) for i in range(100)], True, kernel="tcgen05", seed=33)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_more_sequences_than_are_ranked(causal):
+    check(0, 64, 2, 1, [(0 if i % 11 == 5 else 1 + i * 53 % 200, 1 + i * 29 % 300) for i in range(700)], causal, kernel="tcgen05", seed=34)
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads,count", [(64, 4, 4, 6), (128, 8, 2, 3)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_long_units(dim, heads, kv_heads, count, causal):
+    check(0, dim, heads, kv_heads, [(1500, 1500), (577, 577), (700, 1900), (1900, 700), (2111, 2111)] * count, causal, kernel="tcgen05", seed=35)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_units_with_growing_scores(dim, causal):
+    """Rows whose maximum keeps rising by more than the lag that the kernel allows: their sums and outputs are taken down."""
+    from paper_2507_14959_b200 import binding
+    n, heads = 1024, 10
+    assert binding.attention_packed_kernel(heads=heads, kv_heads=heads, head_dim=dim, n_seqs=2, max_q=n, max_kv=n)[0] == "tcgen05"
+    q, k, v = (normal(40 + i, 2 * n, heads, dim) for i in range(3))
+    k = k * (1 + torch.arange(2 * n).view(-1, 1, 1) % n / 60.0)                # keys grow along the sequence: 1 to 18 times
+    q[5::7] *= 4
+    q, k, v = (x.bfloat16().cuda() for x in (q, k, v))
+    out, status = torch.zeros_like(q), ints([0])
+    binding.attention_packed(q, k, v, out, ints([0, n, 2 * n]), n, n, 0, causal=causal, status=status)
+    assert status.item() == 0
+    for a in (0, n):
+        want, mean, size = expected(q[a:a + n], k[a:a + n], v[a:a + n], causal, dim ** -0.5)
+        error, limit = (out[a:a + n].double() - want).abs(), bound(0, want, mean, size, dim, n)
+        assert (error <= limit).all(), (error / limit).max()
+
+
+def test_values_that_are_not_numbers_stay_in_their_rows():
+    """A NaN in a query is in its row's output alone, one in a key in the outputs of the rows that see it; hidden keys may hold anything."""
+    from paper_2507_14959_b200 import binding
+    for n, seqs, kernel in ((40, 1, "16 rows"), (300, 12, "tcgen05")):
+        heads, dim = 4, 64
+        assert binding.attention_packed_kernel(heads=heads, kv_heads=heads, head_dim=dim, n_seqs=seqs, max_q=n, max_kv=n)[0] == kernel
+        q, k, v = (normal(50 + i, seqs * n, heads, dim).bfloat16().cuda() for i in range(3))
+        off, out = ints([i * n for i in range(seqs + 1)]), torch.zeros_like(q)
+        binding.attention_packed(q, k, v, out, off, n, n, 0, causal=True)
+        plain = out.clone()
+        q[7, 1] = math.nan
+        k[n - 3, 2] = math.nan
+        binding.attention_packed(q, k, v, out, off, n, n, 0, causal=True)
+        bad = torch.zeros_like(out, dtype=torch.bool)
+        bad[7, 1] = True
+        bad[n - 3:n, 2] = True
+        assert torch.isnan(out[bad]).all() and torch.equal(out[~bad], plain[~bad])
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("queries", [1, 3])
+def test_a_long_history_shared_through_a_workspace(dim, queries):
+    check(0, dim, 16, 4, [(queries, 20001)], True, slots=True, gap=7, kernel="workspace", seed=61)
+    check(0, dim, 4, 2, [(queries, 9000), (0, 0), (queries, 17), (queries, 0)], True, slots=True, gap=7, kernel="workspace", seed=62)
+    check(0, dim, 4, 2, [(queries, 5001), (queries, 4444)], False, kernel="workspace", seed=63)
+
+
+def test_a_workspace_that_is_too_small_or_missing():
+    """The library itself: with less than it asks for it takes clusters, with enough the workspace; nothing behind it is written."""
+    import ctypes as C
+    from paper_2507_14959_b200 import binding
+    lib, heads, kv_heads, dim, n = binding.load(), 8, 2, 64, 12000
+    q, k, v = normal(1, 1, heads, dim).bfloat16().cuda(), normal(2, n, kv_heads, dim).bfloat16().cuda(), normal(3, n, kv_heads, dim).bfloat16().cuda()
+    q_off, k_off = ints([0, 1]), ints([0, n])
+    want, mean, size = expected(q, k, v, True, dim ** -0.5)
+    limit = bound(0, want, mean, size, dim, n)
+
+    def args(space, count):
+        out = torch.full_like(q, FILL)
+        return out, binding._ATTENTION_ARGS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), heads * dim, kv_heads * dim, kv_heads * dim, heads * dim,
+                                                 q_off.data_ptr(), k_off.data_ptr(), 0, 1, n, 1, 1, n, heads, kv_heads, dim, 1, 0.0, 0, 0, space, count)
+    need = C.c_size_t(0)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert lib.pm_attention_packed_workspace(args(0, 0)[1], sms, C.byref(need)) == 0 and need.value > 0
+    for have in (0, 16, need.value - 16, need.value):
+        space = torch.full((need.value + 4096,), 77, dtype=torch.uint8, device="cuda")
+        out, packed = args(space.data_ptr() if have else 0, have)
+        assert lib.pm_attention_packed(packed, binding._stream_ptr(None)) == 0
+        torch.cuda.synchronize()
+        assert ((out.double() - want).abs() <= limit).all(), have
+        assert (space[need.value:] == 77).all() and ((space[:need.value] == 77).all().item() == (have < need.value))
+
+
+def test_graphs_replayed_side_by_side_share_no_workspace():
+    from paper_2507_14959_b200 import binding
+    n, heads, kv_heads, dim = 15000, 8, 2, 128
+    streams, graphs, calls = [torch.cuda.Stream(), torch.cuda.Stream()], [], []
+    for i, s in enumerate(streams):
+        q, k, v = normal(i, 1, heads, dim).bfloat16().cuda(), normal(10 + i, n, kv_heads, dim).bfloat16().cuda(), normal(20 + i, n, kv_heads, dim).bfloat16().cuda()
+        out, q_off, k_off = torch.zeros_like(q), ints([0, 1]), ints([0, n])
+        call = lambda q=q, k=k, v=v, out=out, q_off=q_off, k_off=k_off: binding.attention_packed(q, k, v, out, q_off, 1, n, 0, kv_offsets=k_off, causal=True)  # noqa: E731
+        with torch.cuda.stream(s):
+            call()
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                call()
+        graphs.append((g, call))                       # the call's buffers, its lists among them, outlive the replays
+        calls.append((q, k, v, out))
+    for turn in range(20):
+        for q, k, v, out in calls:
+            q.copy_(normal(100 + turn, *q.shape))
+            out.zero_()
+        torch.cuda.synchronize()
+        for s, (g, _) in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        if turn % 5 == 0:
+            for q, k, v, out in calls:
+                want, mean, size = expected(q, k, v, True, dim ** -0.5)
+                assert ((out.double() - want).abs() <= bound(0, want, mean, size, dim, n)).all()
 
 
 @pytest.mark.parametrize("dtype", [0, 1])

@@ -161,3 +161,55 @@ def test_the_binding_reads_shapes_and_distances(lib):
     for bad in (qkv[:, ::2], qkv[..., ::2], qkv.transpose(1, 2), qkv[0]):
         with pytest.raises(binding.PolymorphError):
             binding._heads("x", "q", bad)
+
+
+# ---- which kernel a call takes ---------------------------------------------------------------------
+@pytest.mark.parametrize("sizes,form", [
+    # one frame: tiles of 16 rows; sixteen: units of 256
+    (dict(heads=12, kv_heads=12, head_dim=64, n_seqs=1, max_q=197, max_kv=197), ("16 rows", 1, 1)),
+    (dict(heads=12, kv_heads=12, head_dim=64, n_seqs=16, max_q=197, max_kv=197), ("tcgen05", 1, 1)),
+    (dict(heads=12, kv_heads=12, head_dim=64, n_seqs=64, max_q=577, max_kv=577), ("tcgen05", 1, 1)),
+    # single tokens: shared by a cluster, by the whole GPU with a workspace, or in even shares of many streams
+    (dict(heads=16, kv_heads=4, head_dim=128, n_seqs=1, max_q=1, max_kv=32000), ("16 rows", 8, 1)),
+    (dict(heads=16, kv_heads=4, head_dim=128, n_seqs=1, max_q=1, max_kv=32000, workspace_bytes=1 << 24), ("16 rows", 1, 74)),
+    (dict(heads=16, kv_heads=4, head_dim=128, n_seqs=1, max_q=1, max_kv=32000, workspace_bytes=1 << 10), ("16 rows", 8, 1)),
+    (dict(heads=32, kv_heads=8, head_dim=128, n_seqs=48, max_q=1, max_kv=8192), ("16 rows", 4, 1)),
+    (dict(heads=32, kv_heads=8, head_dim=128, n_seqs=48, max_q=1, max_kv=300), ("16 rows", 1, 1)),
+    (dict(heads=32, kv_heads=8, head_dim=128, n_seqs=3, max_q=8192, max_kv=8192), ("tcgen05", 1, 1)),
+    (dict(heads=6, kv_heads=6, head_dim=64, n_seqs=8, max_q=577, max_kv=577, dtype=1), ("fp32", 2, 1)),
+    (dict(heads=6, kv_heads=6, head_dim=64, n_seqs=8, max_q=0, max_kv=577), ("none", 1, 1))])
+def test_kernel_of_a_call(lib, sizes, form):
+    assert binding.attention_packed_kernel(**sizes) == form
+
+
+def test_kernel_and_workspace_refuse(lib):
+    form, need = (C.c_int32 * 3)(), C.c_size_t(0)
+    good = bytes(attention())
+    assert lib.pm_attention_packed_kernel(good, 148, None) == lib.pm_attention_packed_kernel(good, 0, form) == binding.PM_ERR_ARG
+    assert lib.pm_attention_packed_workspace(good, 148, None) == lib.pm_attention_packed_workspace(good, -1, C.byref(need)) == binding.PM_ERR_ARG
+    bad = bytes(attention(head_dim=96))
+    assert lib.pm_attention_packed_kernel(bad, 148, form) == lib.pm_attention_packed_workspace(bad, 148, C.byref(need)) == binding.PM_ERR_ARG
+    assert lib.pm_attention_packed(bytes(attention(workspace=ADDRESS + 8, workspace_bytes=64)), None) == binding.PM_ERR_ARG
+
+
+def test_the_binding_asks_for_every_workspace_that_is_of_use(lib):
+    """The sizes at which the binding asks cover all those at which the library has a use for one."""
+    need, useful = C.c_size_t(0), 0
+    for heads, kv_heads in ((1, 1), (16, 4), (64, 1), (12, 12)):
+        for n in (1, 2, 5, 20):
+            for max_q in (1, 2, 9, 40):
+                for max_kv in (1000, 4095, 4096, 9000, 100000):
+                    a = attention(heads=heads, kv_heads=kv_heads, q_stride=heads * 64, out_stride=heads * 64, k_stride=kv_heads * 64, v_stride=kv_heads * 64, n_seqs=n,
+                                  q_rows=n * max_q, kv_rows=n * max_kv, max_q=max_q, max_kv=max_kv)
+                    assert lib.pm_attention_packed_workspace(bytes(a), 148, C.byref(need)) == 0
+                    if need.value:
+                        useful += 1
+                        assert max_kv >= binding.LONG_HISTORY and n * kv_heads * ((max_q * (heads // kv_heads) + 15) // 16) <= binding.FEW_TILES
+    assert useful > 20
+
+
+def test_the_structs_are_packed_as_the_library_reads_them(lib):
+    for cls, pack in ((binding.pm_packed_attention, binding._ATTENTION_ARGS), (binding.pm_qk_norm_rope_args, binding._NORM_ARGS)):
+        values = [float(i) if t is C.c_float else i for i, (_, t) in enumerate(cls._fields_, 1)]
+        read = cls.from_buffer_copy(pack.pack(*values))
+        assert [getattr(read, n) for n, _ in cls._fields_] == values
