@@ -474,7 +474,7 @@ typedef struct {
     int32_t* status_out;                  /* dev int32 or NULL: cleared by the call; PM_ERR_ARG if a sequence's offsets or length are
                                              malformed, lie outside the buffers or exceed max_q / max_kv (the sequence is skipped, its
                                              rows of out left as they were), PM_ERR_TIMEOUT if a bounded wait expired */
-    void* workspace;                      /* dev, 16-byte aligned, or NULL; see pm_attention_packed_workspace  */
+    void* workspace;                      /* dev, 32-byte aligned, or NULL; see pm_attention_packed_workspace  */
     size_t workspace_bytes;
 } pm_packed_attention;
 
@@ -484,16 +484,16 @@ typedef struct {
  * PM_ERR_CUDA.  Nothing is launched on error. */
 int pm_attention_packed(const pm_packed_attention* args, void* cuda_stream);
 
-/* Host function (needs no GPU; n_sms: multiprocessors of the one that will run the call): bytes of workspace with which the call's few rows
- * share a long history among all of the GPU; 0 for most calls.  With less, or none, the call takes up to eight CTAs per 16 rows of a K/V head
- * (45 against 18.5 us for one token of 16 heads over 32000 keys of 4 heads of 128).  The contents need not be kept; two calls that may overlap
+/* Host function (needs no GPU; n_sms: multiprocessors of the one that will run the call): bytes of workspace with which calls of few rows, or of
+ * too few to fill the GPU evenly, share their long histories among all of it; 0 for most calls.  With less, or none, such a call takes what it
+ * can without (45 against 18.5 us for one token of 16 heads over 32000 keys of 4 heads of 128).  The contents need not be kept; two calls that may overlap
  * -- on different streams, or in graphs replayed side by side -- need a workspace each. */
 int pm_attention_packed_workspace(const pm_packed_attention* args, int n_sms, size_t* bytes);
 
 /* Which kernel a call takes on a GPU of n_sms multiprocessors (library diagnostics; nothing is launched and no GPU is needed).
  *   form[0]  0 = tiles of 16 rows (few rows, small calls), 1 = tcgen05, units of 256 rows, 2 = fp32; -1 = nothing to do
  *   form[1]  CTAs of a cluster that share the keys of a row tile
- *   form[2]  CTAs that share them through the workspace */
+ *   form[2]  CTAs (0) or units (1) that share them through the workspace */
 int pm_attention_packed_kernel(const pm_packed_attention* args, int n_sms, int32_t* form);
 
 #ifdef __cplusplus

@@ -629,8 +629,8 @@ def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_be
         raise PolymorphError(rc, where)
 
 
-LONG_HISTORY = 4096            # keys below which, and tiles of 16 rows above which, no call has a use for a workspace
-FEW_TILES = 32
+# no call has a use for a workspace with fewer keys, or with more units of 128 rows
+LONG_HISTORY, MANY_UNITS = 512, 4096
 
 
 def _workspace(lib, args, like, stream):
@@ -680,7 +680,7 @@ def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offset
     fields = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), qs, ks, v_shape[3], o_shape[3], qo, ko, kl, rows, kv_rows, n, max_q, max_kv, heads,
               kv_heads, dim, 1 if causal else 0, 0.0 if scale is None else scale, dtype, sp)
     args = _ATTENTION_ARGS.pack(*fields, 0, 0)
-    if max_kv >= LONG_HISTORY and dtype == 0 and n * kv_heads * ((max_q * (heads // kv_heads) + 15) // 16) <= FEW_TILES:
+    if max_kv >= LONG_HISTORY and dtype == 0 and (n * kv_heads + rows * heads // 128) <= MANY_UNITS:
         space = _workspace(lib, args, q, stream)
         if space is not None:
             args = _ATTENTION_ARGS.pack(*fields, space.data_ptr(), space.numel())

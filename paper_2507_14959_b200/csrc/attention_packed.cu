@@ -569,22 +569,41 @@ RowsForm rows_form(const PackedArgs& a, int n_sms, bool workspace) {
     }
     return f;
 }
-// Whether 16-row tiles serve, by what both kernels take in us as measured on a B200 (twenty shapes of 1 to 256 sequences, 16 to 1024 rows per K/V
-// head and 17 to 16000 keys: within a third of either kernel's time, and the faster one is chosen in every one of them).
+// What both kernels take, in us, as measured on a B200 (twenty shapes of 1 to 256 sequences, 16 to 1024 rows per K/V head and 17 to 16000 keys:
+// within a third of either kernel's time, and the faster one is chosen in every one of them).
 //   16-row tiles:  3, joining 2 (4 through a workspace); a CTA 0.55 and per 16 keys 0.07 (head dim 64) or 0.15 (128) beside another on its
 //                  multiprocessor, 1.6 times that alone
-//   tcgen05:       5; a unit of 256 rows 1.3 and per block of 64 keys 0.76, whatever its rows: two tiles' chains of dependent steps
-// Lengths are the call's limits, or what the buffers hold per sequence.
-bool few_rows(const PackedArgs& a, int head_dim, const RowsForm& f, int n_sms) {
-    if (a.kv_rows == 0) return true;
-    const double seqs = a.n_seqs, rows = std::min(seqs * a.max_q, (double)a.q_rows) * a.group, keys = std::min((double)a.max_kv, a.kv_rows / seqs);
-    const double share = (double)f.cluster * f.splits, ctas = std::min(seqs * f.tiles, rows / 16 + seqs) * a.kv_heads * share;
+//   tcgen05:       5, joining 4 and what the parts take at 4 TB/s; a unit of 256 rows 1.3 and per block of 64 keys 0.76, whatever its rows: two
+//                  tiles' chains of dependent steps.  Units of unequal length (causal order) fill the multiprocessors by falling length, equal ones in rounds,
+//                  and the longest one is a bound.
+// Lengths are the call's limits, or what the buffers hold per sequence; in causal order a query sees all keys but half of the queries' on average.
+struct PackedWork { double seqs, queries, keys, seen; };
+PackedWork packed_work(const PackedArgs& a) {
+    const double seqs = a.n_seqs, queries = std::min(seqs * a.max_q, (double)a.q_rows), keys = std::min((double)a.max_kv, a.kv_rows / seqs);
+    return {seqs, queries, keys, a.causal ? keys - std::min(keys, queries / seqs) / 2 : keys};
+}
+double rows_time(const PackedArgs& a, int head_dim, const RowsForm& f, int n_sms) {
+    const PackedWork w = packed_work(a);
+    const double share = (double)f.cluster * f.splits, ctas = std::min(w.seqs * f.tiles, w.queries * a.group / 16 + w.seqs) * a.kv_heads * share;
     const double per_16 = (head_dim == 64 ? 0.07 : 0.15) * (ctas < n_sms ? 1.6 : 1.0);
-    const double t_rows = 3.0 + (f.splits > 1 ? 4.0 : f.cluster > 1 ? 2.0 : 0.0) + std::max(ctas / n_sms, 1.0) * (0.55 + per_16 * keys / (16.0 * share));
+    return 3.0 + (f.splits > 1 ? 4.0 : f.cluster > 1 ? 2.0 : 0.0) + std::max(ctas / n_sms, 1.0) * (0.55 + per_16 * w.seen / (16.0 * share));
+}
+double tc_time(const PackedArgs& a, int head_dim, int splits, int n_sms) {
+    const PackedWork w = packed_work(a);
     const double per_unit = PACKED_TC_ROWS / a.group * a.group;
-    const double units = std::min(seqs * ceil((double)a.max_q * a.group / per_unit), rows / per_unit + seqs) * a.kv_heads;
-    const double t_tc = 5.0 + ceil(units / n_sms) * (1.3 + 0.76 * ceil(keys / 64.0));
-    return t_rows < t_tc;
+    const double units = std::min(w.seqs * ceil((double)a.max_q * a.group / per_unit), w.queries * a.group / per_unit + w.seqs) * a.kv_heads * splits;
+    auto unit = [&](double keys) { return 1.3 + 0.76 * ceil(ceil(keys / 64.0) / splits); };
+    const double run = std::max(unit(a.max_kv), w.seen < w.keys ? units / n_sms * unit(w.seen) : ceil(units / n_sms) * unit(w.keys));
+    return 5.0 + run + (splits > 1 ? 4.0 + (double)packed_tc_workspace(a, head_dim, splits) * 2 / 4e6 : 0.0);
+}
+// units that share a tile pair's keys, with a workspace of that size
+constexpr int TC_MAX_SPLITS = 8;
+constexpr size_t TC_MAX_WORKSPACE = (size_t)256 << 20;
+int tc_splits(const PackedArgs& a, int head_dim, int n_sms, size_t bytes) {
+    int best = 1;
+    for (int s = 2; s <= TC_MAX_SPLITS; ++s)
+        if (packed_tc_workspace(a, head_dim, s) <= std::min(bytes, TC_MAX_WORKSPACE) && tc_time(a, head_dim, s, n_sms) < 0.9 * tc_time(a, head_dim, best, n_sms)) best = s;
+    return best;
 }
 size_t rows_workspace(const PackedArgs& a, int head_dim, const RowsForm& f) {
     if (f.splits == 1) return 0;
@@ -632,11 +651,14 @@ bool heads_ok(const void* p, long long stride, int heads, int dim, int dtype) {
 
 namespace {
 
-// Whether 16-row tiles serve a bf16 call with the workspace it has, and their form.
-bool bf16_form(const pm_packed_attention* p, const PackedArgs& a, int n_sms, RowsForm& f) {
-    f = rows_form(a, n_sms, p->workspace != nullptr);
-    if (p->workspace_bytes < rows_workspace(a, p->head_dim, f)) f = rows_form(a, n_sms, false);
-    return few_rows(a, p->head_dim, f, n_sms);
+// Whether 16-row tiles serve a bf16 call with that much workspace; their form, and the units that share keys otherwise.
+bool bf16_form(const PackedArgs& a, int head_dim, int n_sms, size_t bytes, RowsForm& f, int& splits) {
+    f = rows_form(a, n_sms, true);
+    if (bytes < rows_workspace(a, head_dim, f)) f = rows_form(a, n_sms, false);
+    splits = 1;
+    if (a.kv_rows == 0) return true;
+    splits = tc_splits(a, head_dim, n_sms, bytes);
+    return rows_time(a, head_dim, f, n_sms) < tc_time(a, head_dim, splits, n_sms);
 }
 
 // Checks everything the host can see; PM_OK with nothing to do leaves a.n_seqs 0.
@@ -650,7 +672,7 @@ int packed_args(const pm_packed_attention* p, PackedArgs& a) {
     a = PackedArgs{};
     if (p->n_seqs == 0 || p->q_rows == 0 || p->max_q == 0) return PM_OK;
     if (!heads_ok(p->q, p->q_stride, p->heads, p->head_dim, p->dtype) || !heads_ok(p->out, p->out_stride, p->heads, p->head_dim, p->dtype) ||
-        !p->q_offsets || (p->kv_lengths && !p->kv_offsets) || ((uintptr_t)p->workspace & 15))
+        !p->q_offsets || (p->kv_lengths && !p->kv_offsets) || ((uintptr_t)p->workspace & 31))
         return PM_ERR_ARG;
     if (p->kv_rows > 0 && (!heads_ok(p->k, p->k_stride, p->kv_heads, p->head_dim, p->dtype) ||
                            !heads_ok(p->v, p->v_stride, p->kv_heads, p->head_dim, p->dtype)))
@@ -675,8 +697,9 @@ int pm_attention_packed_workspace(const pm_packed_attention* p, int n_sms, size_
     if (const int rc = packed_args(p, a); rc != PM_OK) return rc;
     *bytes = 0;
     if (a.n_seqs > 0 && p->dtype == 0) {
-        const RowsForm f = rows_form(a, n_sms, true);
-        if (few_rows(a, p->head_dim, f, n_sms)) *bytes = rows_workspace(a, p->head_dim, f);
+        RowsForm f;
+        int splits;
+        *bytes = bf16_form(a, p->head_dim, n_sms, SIZE_MAX, f, splits) ? rows_workspace(a, p->head_dim, f) : packed_tc_workspace(a, p->head_dim, splits);
     }
     return PM_OK;
 }
@@ -693,8 +716,12 @@ int pm_attention_packed_kernel(const pm_packed_attention* p, int n_sms, int32_t*
         return PM_OK;
     }
     RowsForm f;
-    form[0] = bf16_form(p, a, n_sms, f) ? 0 : 1;
-    if (form[0] == 0) { form[1] = f.cluster; form[2] = f.splits; }
+    int splits;
+    if (bf16_form(a, p->head_dim, n_sms, p->workspace ? p->workspace_bytes : 0, f, splits)) {
+        form[0] = 0; form[1] = f.cluster; form[2] = f.splits;
+    } else {
+        form[0] = 1; form[2] = splits;
+    }
     return PM_OK;
 }
 
@@ -718,14 +745,15 @@ int pm_attention_packed(const pm_packed_attention* p, void* cuda_stream) {
     L.status = a.status;
     cudaError_t e;
     RowsForm f;
+    int splits = 1;
     if (p->dtype == 1) {
         const F32Form f = f32_form(a, n_sms);
         e = p->head_dim == 64 ? (f.rows == 16 ? launch_f32<64, 16>(L, a, f) : launch_f32<64, 64>(L, a, f))
                               : (f.rows == 16 ? launch_f32<128, 16>(L, a, f) : launch_f32<128, 64>(L, a, f));
-    } else if (bf16_form(p, a, n_sms, f)) {
+    } else if (bf16_form(a, p->head_dim, n_sms, p->workspace ? p->workspace_bytes : 0, f, splits)) {
         e = p->head_dim == 64 ? launch_rows<64>(L, a, f, p->workspace) : launch_rows<128>(L, a, f, p->workspace);
     } else {
-        e = launch_packed_tc(L, a, p->head_dim, n_sms);
+        e = launch_packed_tc(L, a, p->head_dim, n_sms, splits, p->workspace);
     }
     return e == cudaSuccess ? PM_OK : PM_ERR_CUDA;
 }

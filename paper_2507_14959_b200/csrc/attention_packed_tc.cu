@@ -43,21 +43,26 @@ template <int D>
 struct PtLayout {
     static constexpr uint32_t TMEM = 512;
     static constexpr int Q_BYTES = PT_ROWS * D * 2, KV_BYTES = PT_KEYS * D * 2;       // of a tile's queries, of a K or V block
-    static constexpr int Q_SLOTS = D == 64 ? 4 : 3, KV_SLOTS = D == 64 ? 12 : 7;
+    // Query tiles in turn, a ring for each tile: a wait tells one phase of a barrier from the next only, so whoever waits on a slot has to be the one
+    // whose signal frees it.
+    static constexpr int Q_SLOTS = 4, KV_SLOTS = D == 64 ? 12 : 5;
+    static __host__ __device__ constexpr uint32_t q_slot(int i, uint32_t use) { return 2 * i + use % 2; }
     // a tile's columns: two buffers of scores, O
     static __host__ __device__ constexpr uint32_t s_col(int i, uint32_t buffer) { return i * 256 + buffer * PT_KEYS; }
     static __host__ __device__ constexpr uint32_t o_col(int i) { return i * 256 + 2 * PT_KEYS; }
 };
 
-struct PtUnit {                                               // 32 bytes
+struct __align__(16) PtUnit {
     int q0, nq, k0, nk;                                       // the sequence
     int tok0, kv_head, blocks0, blocks1;                      // first query; key blocks of the two tiles; blocks0 < 0: no more units
+    int first, part, pad[2];                                  // first key block; which of the units that share the keys
 };
 
 template <int D>
 struct PtControl {
     Segment sorted[PT_SORTED];                                // by falling cost
-    int before[PT_SORTED];                                    // units of the sequences ahead of it
+    int before[PT_SORTED];                                    // units of the sequences ahead of it; in causal order the level of its first unit
+    int many[PT_SORTED];                                      // its units
     int key[PT_SORTED], count[PT_SORTED];                     // in the caller's order: cost, units
     PtUnit units[PT_UNITS];
     unsigned long long q_full[PtLayout<D>::Q_SLOTS], q_empty[PtLayout<D>::Q_SLOTS];
@@ -77,6 +82,10 @@ static_assert(pt_smem<64>() <= 227 * 1024 && pt_smem<128>() <= 227 * 1024, "shar
 struct PtArgs {
     PackedArgs a;
     int tile_tokens;                                          // TT
+    // parts of shared keys, at (part * q_rows + row) * heads + head: output before the division, row maximum (times c) and sum
+    int splits;
+    float* part_o;
+    float2* part_ml;
 };
 
 // Bounded wait in which the hardware lets the warp sleep, after a look that costs less than falling asleep.
@@ -152,7 +161,7 @@ __device__ __forceinline__ int round16(int n) { return (n + 15) & ~15; }
 // lands on a barrier of its own, where warp 10 awaits it, and passes it on to those who await the ring.
 __device__ __forceinline__ bool has_tail(const PtUnit& u) {
     const int blocks = max(u.blocks0, u.blocks1);
-    return blocks * PT_KEYS > u.nk && (u.nk & 15) != 0;
+    return blocks > 0 && (u.first + blocks) * PT_KEYS > u.nk && (u.nk & 15) != 0;
 }
 
 // Key blocks of a tile whose first query is `tok` (0: no queries, or none of them sees a key).
@@ -163,10 +172,10 @@ __device__ __forceinline__ int tile_blocks(const Segment& g, int tok, int tile_t
 // Keys of block j that the tile's last query sees, at most a block.
 __device__ __forceinline__ int block_keys(const PtUnit& u, int tile, int j, int tile_tokens, int causal) {
     const Segment g{u.q0, u.nq, u.k0, u.nk};
-    return min(PT_KEYS, packed_visible(g, min(u.tok0 + (tile + 1) * tile_tokens, u.nq) - 1, causal) - j * PT_KEYS);
+    return min(PT_KEYS, packed_visible(g, min(u.tok0 + (tile + 1) * tile_tokens, u.nq) - 1, causal) - (u.first + j) * PT_KEYS);
 }
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ void __launch_bounds__(PT_THREADS, 1)
 attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                            const __grid_constant__ PtArgs args) {
@@ -211,12 +220,13 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     const int per_unit = 2 * TT;
     if (ranked) {
         Segment g{0, 0, 0, 0};
-        int key = 0, count = 0;
+        int key = 0, count = 0, low = 0;
         const int me = (int)threadIdx.x;
         if (me < a.n_seqs) {
             g = packed_segment(a, me);
             count = (g.nq + per_unit - 1) / per_unit;
-            key = a.causal ? count : g.nk;
+            low = max(0, g.nk - g.nq) / per_unit;
+            key = a.causal ? low + count : g.nk;
             ctl.key[me] = key;
             ctl.count[me] = count;
         }
@@ -228,7 +238,8 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 if (other > key || (other == key && k < me)) { ++rank; before += ctl.count[k]; }
             }
             ctl.sorted[rank] = g;
-            ctl.before[rank] = before;
+            ctl.before[rank] = a.causal ? low : before;
+            ctl.many[rank] = count;
         }
     }
     tc_fence_before();
@@ -240,8 +251,8 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     auto take_unit = [&](uint32_t n, PtUnit& u) {
         if (!wait_asleep(bar(ctl.unit_full[n % PT_UNITS]), (n / PT_UNITS) & 1u, abort_flag, a.status)) return false;
         const int4* p = reinterpret_cast<const int4*>(&ctl.units[n % PT_UNITS]);
-        const int4 x = p[0], y = p[1];
-        u = PtUnit{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        const int4 x = p[0], y = p[1], z = SPLIT ? p[2] : make_int4(0, 0, 0, 0);
+        u = PtUnit{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, {0, 0}};
         return true;
     };
 
@@ -259,7 +270,8 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
         for (uint32_t n = 0; ok; ++n) {
             int blocks, vis, vis_all;                         // vis_all: keys that every row sees
             bool real;
-            bf16* to;                                         // this thread's row of the output
+            bf16* to;                                         // this thread's row of the output, or of its part
+            long long part = 0;
             {
                 PtUnit u;
                 ok = take_unit(n, u);
@@ -269,10 +281,11 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 blocks = tile ? u.blocks1 : u.blocks0;
                 const Segment seg{u.q0, u.nq, u.k0, u.nk};
                 const int tok0 = u.tok0 + tile * TT;
-                vis = packed_visible(seg, min(tok0 + row_tok, u.nq - 1), a.causal);
-                vis_all = packed_visible(seg, tok0, a.causal);
+                vis = packed_visible(seg, min(tok0 + row_tok, u.nq - 1), a.causal) - u.first * PT_KEYS;
+                vis_all = packed_visible(seg, tok0, a.causal) - u.first * PT_KEYS;
                 real = row_tok < TT && tok0 + row_tok < u.nq;
                 to = (bf16*)a.out + (long long)(u.q0 + tok0 + row_tok) * a.out_stride + u.kv_head * a.group * D + head_at;
+                if (SPLIT) part = ((long long)u.part * a.q_rows + u.q0 + tok0 + row_tok) * a.heads + u.kv_head * a.group + row % a.group;
                 if (u.blocks0 < 0) break;
             }
             float m = -INFINITY;
@@ -350,7 +363,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 if (lane == 0) mbar_arrive(bar(ctl.p_ready[tile][buffer]));
             }
             if (!ok) break;
-            float inv = 0.f;
+            float inv = 0.f, l = 0.f;
             if (blocks > 0) {
                 ok = wait_asleep(bar(ctl.o_ready[tile]), tiles & 1u, abort_flag, a.status);
                 ++tiles;
@@ -359,29 +372,51 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 tc_fence_after();
                 float x, y;
                 upk2(add2(sum0, sum1), x, y);
-                inv = x + y == 0.f ? 0.f : 1.f / (x + y);
+                l = x + y;
+                inv = l == 0.f ? 0.f : 1.f / l;
             }
-#pragma unroll
-            for (int k = 0; k < D; k += 32) {
-                uint32_t o[32];
+            if constexpr (SPLIT) {
+                // -inf and 0 if this part sees nothing, and then its output is not read; not so if its sum is no number
+                if (real) args.part_ml[part] = make_float2(l == l ? m * c : 0.f, l);
                 if (blocks > 0) {
-                    tmem_ld32(t_o + k, o);
-                    tmem_ld_wait();
-                } else {
+                    float* po = args.part_o + part * D;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    for (int k = 0; k < D; k += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(t_o + k, o);
+                        tmem_ld_wait();
+                        if (real)
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8)
+                                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                                             ::"l"(po + k + e), "r"(o[e]), "r"(o[e + 1]), "r"(o[e + 2]), "r"(o[e + 3]), "r"(o[e + 4]), "r"(o[e + 5]), "r"(o[e + 6]),
+                                               "r"(o[e + 7])
+                                             : "memory");
+                    }
                 }
+            } else {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
-                if (real && sectors) {
+                for (int k = 0; k < D; k += 32) {
+                    uint32_t o[32];
+                    if (blocks > 0) {
+                        tmem_ld32(t_o + k, o);
+                        tmem_ld_wait();
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8)
-                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                                     ::"l"(to + k + 2 * e), "r"(o[e]), "r"(o[e + 1]), "r"(o[e + 2]), "r"(o[e + 3]), "r"(o[e + 4]), "r"(o[e + 5]), "r"(o[e + 6]), "r"(o[e + 7])
-                                     : "memory");
-                } else if (real) {
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    }
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + k + 2 * e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    for (int e = 0; e < 16; ++e) o[e] = pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+                    if (real && sectors) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8)
+                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                                         ::"l"(to + k + 2 * e), "r"(o[e]), "r"(o[e + 1]), "r"(o[e + 2]), "r"(o[e + 3]), "r"(o[e + 4]), "r"(o[e + 5]), "r"(o[e + 6]), "r"(o[e + 7])
+                                         : "memory");
+                    } else if (real) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(to + k + 2 * e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    }
                 }
             }
             // O is in registers before the next unit's first P is announced, and that comes before the product that overwrites it
@@ -393,7 +428,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 // -------------------------------------------------------------- MMA issue, a thread for each tile
                 // Steps: key blocks of the units, in order; kv: ring position of a step's K block (V follows it).  A step that the other tile has
                 // alone only passes the ring on -- not before the block has landed, or the signal would count for the slot's use before.
-                struct Step { PtUnit u; int j, blocks, mine; uint32_t kv, q; };
+                struct Step { PtUnit u; int j, blocks, mine; uint32_t kv, q; };                // q: which of the tile's query tiles
                 const int i = warp == 8 ? 0 : 1;
                 const uint32_t idesc_pv = instr_desc_b_mn(D), idesc_s = instr_desc(PT_KEYS), t_o = tmem + Lay::o_col(i);
                 uint32_t units = 0, kv_next = 0, q_next = 0, s_count = 0, p_count = 0;
@@ -419,8 +454,8 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     s.kv = kv_next;
                     kv_next += 2;
                     s.mine = i ? s.u.blocks1 : s.u.blocks0;
-                    if (s.u.blocks0 > 0) { if (i == 0) s.q = q_next; ++q_next; }
-                    if (s.u.blocks1 > 0) { if (i == 1) s.q = q_next; ++q_next; }
+                    s.q = q_next;
+                    if (s.mine > 0) ++q_next;
                     return true;
                 };
                 auto full = [&](uint32_t at) { return wait_asleep(bar(ctl.kv_full[at % Lay::KV_SLOTS]), (at / Lay::KV_SLOTS) & 1u, abort_flag, a.status); };
@@ -431,10 +466,10 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                         mbar_arrive(bar(ctl.kv_empty[k_slot]));
                         return;
                     }
-                    const uint32_t q_slot = s.q % Lay::Q_SLOTS, buffer = s_count++ & 1u, to = tmem + Lay::s_col(i, buffer);
+                    const uint32_t q_slot = Lay::q_slot(i, s.q), buffer = s_count++ & 1u, to = tmem + Lay::s_col(i, buffer);
                     const uint64_t dq = smem_desc(q_s((int)q_slot), 128), dk = smem_desc(kv_s((int)k_slot), 128);
                     const uint32_t idesc = s.j + 1 < s.mine ? idesc_s : instr_desc(round16(block_keys(s.u, i, s.j, TT, a.causal)));
-                    if (s.j == 0) ok = wait_asleep(bar(ctl.q_full[q_slot]), (s.q / Lay::Q_SLOTS) & 1u, abort_flag, a.status);
+                    if (s.j == 0) ok = wait_asleep(bar(ctl.q_full[q_slot]), (s.q >> 1) & 1u, abort_flag, a.status);
                     ok = ok && full(s.kv);
                     if (!ok) return;
                     tc_fence_after();
@@ -489,37 +524,62 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             }
         } else if (warp == 9) {
             // ------------------------------------------------------------------ units and loads
-            // The walk over the units: in causal order level by level, level L holding unit L of each sequence that has one (the sequences with most
-            // units come first, so those are the first `reach`); without it sequence by sequence.  `left` counts K/V heads of units from where the
-            // walk stands; the CTAs take them in turn, there and back, so that none has the longest of every turn.
+            // The walk over the units: in causal order level by level from the highest, a level holding the units that see about as many keys: unit L of a
+            // sequence that begins with a history of h units' length is at level h + L; in a level 32 sequences at a time.  Without causal order sequence
+            // by sequence.  `left` counts K/V heads of units from where the
+            // walk stands (and the parts of each); the CTAs take them in turn, there and back, so that none has the longest of every turn.
             const int n_seqs = a.n_seqs;
+            const uint32_t splits = SPLIT ? (uint32_t)args.splits : 1u, shares = (uint32_t)a.kv_heads * splits;
             auto units_of = [&](const Segment& g) { return (g.nq + per_unit - 1) / per_unit; };
             int level = 0, reach = 0, block = 0;
+            const bool here = ranked && lane < n_seqs;        // the levels of this lane's sequence, of up to 32
+            const int low = here ? ctl.before[lane] : 0, high = here ? low + ctl.many[lane] - 1 : -1;
             Segment mine{0, 0, 0, 0};                         // not ranked: a sequence per lane
             if (!ranked) mine = lane < n_seqs ? packed_segment(a, lane) : mine;
-            else if (a.causal) level = units_of(ctl.sorted[0]) - 1;
-            long long left = blockIdx.x;
-            uint32_t units = 0, kv = 0, q = 0, tails = 0;
+            else if (a.causal) level = ctl.before[0] + ctl.many[0] - 1;
+            uint32_t left = blockIdx.x;                       // all units together are fewer than 2^31 (see the launch)
+            uint32_t units = 0, kv = 0, q0 = 0, q1 = 0, tails = 0;
             bool ok = true;
             while (ok) {
                 Segment g{0, 0, 0, 0};
                 int tile = -1;                                // of the sequence, in units
                 if (ranked && a.causal) {
-                    for (; level >= 0; --level) {
-                        while (reach < n_seqs && units_of(ctl.sorted[reach]) > level) ++reach;
-                        const long long here = (long long)reach * a.kv_heads;
+                    if (n_seqs <= 32) {
+                        // all levels at once that hold the same sequences as this one
+                        while (level >= 0) {
+                            const bool in = low <= level && level <= high;
+                            const uint32_t set = __ballot_sync(0xFFFFFFFFu, in);
+                            const int until = __reduce_max_sync(0xFFFFFFFFu, in ? low - 1 : high < level ? high : -1);
+                            const uint32_t each = __popc(set) * shares, here = each * (uint32_t)(level - until);
+                            if (left < here) {
+                                level -= (int)(left / each);
+                                left %= each;
+                                break;
+                            }
+                            left -= here;
+                            level = until;
+                        }
+                    }
+                    while (level >= 0) {
+                        const int at = block + lane, unit = at < n_seqs ? level - ctl.before[at] : -1;
+                        uint32_t set = __ballot_sync(0xFFFFFFFFu, unit >= 0 && unit < (at < n_seqs ? ctl.many[at] : 0));
+                        const uint32_t here = __popc(set) * shares;
                         if (left < here) {
-                            g = ctl.sorted[left / a.kv_heads];
-                            tile = level;
+                            for (int nth = (int)(left / shares); nth > 0; --nth) set &= set - 1;
+                            const int from = __ffs((int)set) - 1;
+                            g = ctl.sorted[block + from];
+                            tile = __shfl_sync(0xFFFFFFFFu, unit, from);
                             break;
                         }
                         left -= here;
+                        block += 32;
+                        if (block >= n_seqs) { block = 0; --level; }
                     }
                 } else if (ranked) {
-                    const long long at = left / a.kv_heads;   // of all units
+                    const int at = (int)(left / shares);      // of all units
                     while (reach + 1 < n_seqs && ctl.before[reach + 1] <= at) ++reach;
                     g = ctl.sorted[reach];
-                    if (at - ctl.before[reach] < units_of(g)) tile = (int)(at - ctl.before[reach]);
+                    if (at - ctl.before[reach] < ctl.many[reach]) tile = at - ctl.before[reach];
                 } else {
                     while (block < n_seqs) {
                         const int mass = units_of(mine);
@@ -529,9 +589,9 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                             const int y = __shfl_up_sync(0xFFFFFFFFu, sum, x);
                             if (lane >= x) sum += y;
                         }
-                        const long long here = (long long)__shfl_sync(0xFFFFFFFFu, sum, 31) * a.kv_heads;
+                        const uint32_t here = (uint32_t)__shfl_sync(0xFFFFFFFFu, sum, 31) * shares;
                         if (left < here) {
-                            const int nth = (int)(left / a.kv_heads);
+                            const int nth = (int)(left / shares);
                             const int from = __ffs((int)__ballot_sync(0xFFFFFFFFu, sum > nth)) - 1;
                             g = Segment{__shfl_sync(0xFFFFFFFFu, mine.q0, from), __shfl_sync(0xFFFFFFFFu, mine.nq, from), __shfl_sync(0xFFFFFFFFu, mine.k0, from),
                                         __shfl_sync(0xFFFFFFFFu, mine.nk, from)};
@@ -543,14 +603,18 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                         mine = block + lane < n_seqs ? packed_segment(a, block + lane) : Segment{0, 0, 0, 0};
                     }
                 }
-                PtUnit u = {0, 0, 0, 0, 0, 0, -1, -1};
+                PtUnit u = {0, 0, 0, 0, 0, 0, -1, -1, 0, 0, {0, 0}};
                 if (tile >= 0) {
                     u.q0 = g.q0; u.nq = g.nq; u.k0 = g.k0; u.nk = g.nk;
                     u.tok0 = tile * per_unit;
-                    u.kv_head = (int)(left % a.kv_heads);
-                    u.blocks0 = tile_blocks(g, u.tok0, TT, a.causal);
-                    u.blocks1 = tile_blocks(g, u.tok0 + TT, TT, a.causal);
-                    left += 2 * ((units & 1u) ? (long long)blockIdx.x : (long long)gridDim.x - 1 - blockIdx.x) + 1;
+                    u.kv_head = (int)(left % shares / splits);
+                    u.part = SPLIT ? (int)(left % splits) : 0;
+                    const int all0 = tile_blocks(g, u.tok0, TT, a.causal), all1 = tile_blocks(g, u.tok0 + TT, TT, a.causal), all = max(all0, all1);
+                    u.first = SPLIT ? (int)((long long)all * u.part / splits) : 0;
+                    const int end = SPLIT ? (int)((long long)all * (u.part + 1) / splits) : all;
+                    u.blocks0 = max(0, min(all0, end) - u.first);
+                    u.blocks1 = max(0, min(all1, end) - u.first);
+                    left += 2 * ((units & 1u) ? blockIdx.x : gridDim.x - 1 - blockIdx.x) + 1;
                 }
                 const int at = (int)(units % PT_UNITS);
                 ok = wait_asleep(bar(ctl.unit_empty[at]), ((units / PT_UNITS) & 1u) ^ 1u, abort_flag, a.status);
@@ -560,6 +624,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     int4* p = reinterpret_cast<int4*>(&ctl.units[at]);
                     p[0] = make_int4(u.q0, u.nq, u.k0, u.nk);
                     p[1] = make_int4(u.tok0, u.kv_head, u.blocks0, u.blocks1);
+                    if (SPLIT) p[2] = make_int4(u.first, u.part, 0, 0);
                     mbar_arrive(bar(ctl.unit_full[at]));
                 }
                 __syncwarp();
@@ -569,13 +634,14 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 const bool tail = has_tail(u);
                 if (elect_one()) {
                     auto load_q = [&](int i) {
-                        const int slot = (int)(q % Lay::Q_SLOTS);
-                        ok = ok && wait_asleep(bar(ctl.q_empty[slot]), ((q / Lay::Q_SLOTS) & 1u) ^ 1u, abort_flag, a.status);
+                        uint32_t& use = i ? q1 : q0;
+                        const int slot = (int)Lay::q_slot(i, use);
+                        ok = ok && wait_asleep(bar(ctl.q_empty[slot]), ((use >> 1) & 1u) ^ 1u, abort_flag, a.status);
                         if (!ok) return;
                         mbar_expect_tx(bar(ctl.q_full[slot]), (uint32_t)(TT * a.group * D * 2));
                         for (int x = 0; x < D / 64; ++x)
                             tma_load_3d(q_s(slot) + x * PT_ROWS * 128, &tm_q, x * 64, u.kv_head * a.group, u.q0 + u.tok0 + i * TT, bar(ctl.q_full[slot]));
-                        ++q;
+                        ++use;
                     };
                     auto load_kv = [&](const CUtensorMap* tm, int j, unsigned long long* full) {
                         const int slot = (int)(kv % Lay::KV_SLOTS);
@@ -583,7 +649,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                         if (!ok) return;
                         const uint32_t on = full ? bar(*full) : bar(ctl.kv_full[slot]);
                         mbar_expect_tx(on, (uint32_t)Lay::KV_BYTES);
-                        for (int x = 0; x < D / 64; ++x) tma_load_3d(kv_s(slot) + x * PT_KEYS * 128, tm, x * 64, u.kv_head, u.k0 + j * PT_KEYS, on);
+                        for (int x = 0; x < D / 64; ++x) tma_load_3d(kv_s(slot) + x * PT_KEYS * 128, tm, x * 64, u.kv_head, u.k0 + (u.first + j) * PT_KEYS, on);
                         ++kv;
                     };
                     for (int j = 0; j < blocks && ok; ++j) {
@@ -597,7 +663,8 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 // the counters of the lane that loaded
                 kv = __reduce_max_sync(0xFFFFFFFFu, kv);
-                q = __reduce_max_sync(0xFFFFFFFFu, q);
+                q0 = __reduce_max_sync(0xFFFFFFFFu, q0);
+                q1 = __reduce_max_sync(0xFFFFFFFFu, q1);
             }
         } else if (warp == 10) {
             // ------------------------------------------------------------------ values behind a sequence's last key
@@ -618,7 +685,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 ++tails;
-                const int first = u.nk - (blocks - 1) * PT_KEYS, rows = round16(first) - first;
+                const int first = u.nk - (u.first + blocks - 1) * PT_KEYS, rows = round16(first) - first;
                 for (int i = lane; i < rows * D / 8; i += 32) {              // whole rows, so their swizzle does not matter
                     const int r = first + i / (D / 8), c = i % (D / 8);
                     st_shared_v4(kv_s(slot) + (uint32_t)((c / 8) * PT_KEYS * 128 + r * 128 + (c % 8) * 16), make_uint4(0, 0, 0, 0));
@@ -644,28 +711,80 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     }
 }
 
+// Joins the parts of a row: a warp per (query, head).
+constexpr int PT_JOIN_WARPS = 8;
 template <int D>
-cudaError_t launch_tc(const Launch& L, const PackedArgs& a, int n_sms) {
-    PtArgs args;
+__global__ void __launch_bounds__(32 * PT_JOIN_WARPS) attention_join_tc_kernel(const __grid_constant__ PtArgs args) {
+    constexpr int EACH = D / 32;
+    const PackedArgs& a = args.a;
+    const int lane = threadIdx.x & 31;
+    dep_release();
+    dep_wait();
+    const Segment g = packed_segment(a, blockIdx.y);
+    const long long i = (long long)blockIdx.x * PT_JOIN_WARPS + (threadIdx.x >> 5);
+    if (i >= (long long)g.nq * a.heads) return;
+    const long long stride = (long long)a.q_rows * a.heads, at = (long long)g.q0 * a.heads + i;
+    float m = -INFINITY;
+    for (int k = 0; k < args.splits; ++k) m = fmaxf(m, args.part_ml[k * stride + at].x);
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) o[e] = 0.f;
+    for (int k = 0; k < args.splits; ++k) {
+        const float2 ml = args.part_ml[k * stride + at];
+        if (ml.x == -INFINITY) continue;                      // saw nothing, left no output
+        const float f = ex2f(ml.x - base);
+        l = fmaf(ml.y, f, l);
+#pragma unroll
+        for (int e = 0; e < EACH; e += 2) {
+            const float2 x = *reinterpret_cast<const float2*>(args.part_o + (k * stride + at) * D + lane * EACH + e);
+            o[e] = fmaf(x.x, f, o[e]);
+            o[e + 1] = fmaf(x.y, f, o[e + 1]);
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bf16* to = (bf16*)a.out + (g.q0 + i / a.heads) * a.out_stride + i % a.heads * D + lane * EACH;
+#pragma unroll
+    for (int e = 0; e < EACH; e += 2) *reinterpret_cast<uint32_t*>(to + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
+}
+
+template <int D>
+cudaError_t launch_tc(const Launch& L, const PackedArgs& a, int n_sms, int splits, void* workspace) {
+    PtArgs args = {};
     args.a = a;
     args.tile_tokens = PT_ROWS / a.group;
+    args.splits = splits;
+    if (splits > 1) {
+        args.part_o = (float*)workspace;
+        args.part_ml = (float2*)(args.part_o + (size_t)splits * a.q_rows * a.heads * D);
+    }
     CUtensorMap tm_q, tm_k, tm_v;
     if (!tm_encode_3d(&tm_q, a.q, D, a.heads, a.q_rows, D * 2, (uint64_t)a.q_stride * 2, 64, a.group, args.tile_tokens, 128) ||
         !tm_encode_3d(&tm_k, a.k, D, a.kv_heads, a.kv_rows, D * 2, (uint64_t)a.k_stride * 2, 64, 1, PT_KEYS, 128) ||
         !tm_encode_3d(&tm_v, a.v, D, a.kv_heads, a.kv_rows, D * 2, (uint64_t)a.v_stride * 2, 64, 1, PT_KEYS, 128))
         return cudaErrorInvalidValue;
-    static SmemGrant grant;
-    if (cudaError_t e = grant.ensure(attention_packed_tc_kernel<D>, (int)pt_smem<D>()); e != cudaSuccess) return e;
-    const long long units = (a.q_rows / (2 * args.tile_tokens) + (long long)a.n_seqs) * a.kv_heads;      // at most
+    static SmemGrant grant[2];
+    const auto kernel = splits > 1 ? attention_packed_tc_kernel<D, true> : attention_packed_tc_kernel<D, false>;
+    if (cudaError_t e = grant[splits > 1].ensure(kernel, (int)pt_smem<D>()); e != cudaSuccess) return e;
+    const long long units = (a.q_rows / (2 * args.tile_tokens) + (long long)a.n_seqs) * a.kv_heads * splits;         // at most
+    if (units >= 1ll << 31) return cudaErrorInvalidValue;
     ProfScope ps(L, KC_ATTENTION);
-    cudaError_t e = launch_overlapped(L, attention_packed_tc_kernel<D>, dim3((unsigned)std::min<long long>(units, n_sms)), PT_THREADS, pt_smem<D>(), 1, tm_q, tm_k,
+    cudaError_t e = launch_overlapped(L, kernel, dim3((unsigned)std::min<long long>(units, n_sms)), PT_THREADS, pt_smem<D>(), 1, tm_q, tm_k,
                                       tm_v, args);
+    BUMP(L);
+    if (e != cudaSuccess || splits == 1) return e;
+    const long long rows = (long long)a.max_q * a.heads;
+    e = launch_overlapped(L, attention_join_tc_kernel<D>, dim3((unsigned)((rows + PT_JOIN_WARPS - 1) / PT_JOIN_WARPS), a.n_seqs), 32 * PT_JOIN_WARPS, 0, 1, args);
     BUMP(L);
     return e;
 }
 
 }  // namespace
 
-cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim, int n_sms) {
-    return head_dim == 64 ? launch_tc<64>(L, a, n_sms) : launch_tc<128>(L, a, n_sms);
+size_t packed_tc_workspace(const PackedArgs& a, int head_dim, int splits) {
+    return splits > 1 ? (size_t)splits * a.q_rows * a.heads * (head_dim + 2) * sizeof(float) : 0;
+}
+
+cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim, int n_sms, int splits, void* workspace) {
+    return head_dim == 64 ? launch_tc<64>(L, a, n_sms, splits, workspace) : launch_tc<128>(L, a, n_sms, splits, workspace);
 }

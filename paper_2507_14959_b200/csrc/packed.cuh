@@ -16,8 +16,10 @@ struct PackedArgs {
 };
 
 
-// the tcgen05 kernel (attention_packed_tc.cu); a.kv_rows > 0
-cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim, int n_sms);
+// The tcgen05 kernel (attention_packed_tc.cu); a.kv_rows > 0.  splits > 1: that many units share a tile pair's keys and leave their parts in the
+// workspace (packed_tc_workspace bytes), where a second kernel joins them.
+size_t packed_tc_workspace(const PackedArgs& a, int head_dim, int splits);
+cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim, int n_sms, int splits, void* workspace);
 
 namespace {
 

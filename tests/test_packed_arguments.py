@@ -189,7 +189,7 @@ def test_kernel_and_workspace_refuse(lib):
     assert lib.pm_attention_packed_workspace(good, 148, None) == lib.pm_attention_packed_workspace(good, -1, C.byref(need)) == binding.PM_ERR_ARG
     bad = bytes(attention(head_dim=96))
     assert lib.pm_attention_packed_kernel(bad, 148, form) == lib.pm_attention_packed_workspace(bad, 148, C.byref(need)) == binding.PM_ERR_ARG
-    assert lib.pm_attention_packed(bytes(attention(workspace=ADDRESS + 8, workspace_bytes=64)), None) == binding.PM_ERR_ARG
+    assert lib.pm_attention_packed(bytes(attention(workspace=ADDRESS + 16, workspace_bytes=64)), None) == binding.PM_ERR_ARG
 
 
 def test_the_binding_asks_for_every_workspace_that_is_of_use(lib):
@@ -197,14 +197,14 @@ def test_the_binding_asks_for_every_workspace_that_is_of_use(lib):
     need, useful = C.c_size_t(0), 0
     for heads, kv_heads in ((1, 1), (16, 4), (64, 1), (12, 12)):
         for n in (1, 2, 5, 20):
-            for max_q in (1, 2, 9, 40):
-                for max_kv in (1000, 4095, 4096, 9000, 100000):
+            for max_q in (1, 2, 9, 40, 300, 2000, 9000):
+                for max_kv in (200, 511, 512, 1000, 4096, 9000, 100000):
                     a = attention(heads=heads, kv_heads=kv_heads, q_stride=heads * 64, out_stride=heads * 64, k_stride=kv_heads * 64, v_stride=kv_heads * 64, n_seqs=n,
                                   q_rows=n * max_q, kv_rows=n * max_kv, max_q=max_q, max_kv=max_kv)
                     assert lib.pm_attention_packed_workspace(bytes(a), 148, C.byref(need)) == 0
                     if need.value:
                         useful += 1
-                        assert max_kv >= binding.LONG_HISTORY and n * kv_heads * ((max_q * (heads // kv_heads) + 15) // 16) <= binding.FEW_TILES
+                        assert max_kv >= binding.LONG_HISTORY and n * kv_heads + n * max_q * heads // 128 <= binding.MANY_UNITS
     assert useful > 20
 
 
