@@ -19,8 +19,6 @@
 
 namespace {
 
-__device__ int packed_status_word;           // where calls without a status word of their own leave what they find
-
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
@@ -735,11 +733,6 @@ int pm_attention_packed(const pm_packed_attention* p, void* cuda_stream) {
     if (a.n_seqs == 0) return PM_OK;
     if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
     a.status = p->status_out;
-    if (!a.status) {
-        void* word = nullptr;
-        if (cudaGetSymbolAddress(&word, packed_status_word) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
-        a.status = (int*)word;
-    }
     Launch L;
     L.st = st;
     L.status = a.status;

@@ -183,8 +183,9 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t base = smem_u32(smem_raw);
     const PackedArgs& a = args.a;
+    int* const status = packed_status(a);
     if (base & 1023u) {                       // swizzled operands need a 1024-byte aligned window
-        if (threadIdx.x == 0) atomicCAS(a.status, 0, (int)PM_ERR_CUDA);
+        if (threadIdx.x == 0) atomicCAS(status, 0, (int)PM_ERR_CUDA);
         return;
     }
     PtControl<D>& ctl = *reinterpret_cast<PtControl<D>*>(smem_raw + Lay::Q_SLOTS * Lay::Q_BYTES + Lay::KV_SLOTS * Lay::KV_BYTES);
@@ -214,7 +215,6 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
         tmem_alloc(smem_u32(&ctl.tmem), Lay::TMEM);
         tmem_relinquish();
     }
-    dep_release();
     dep_wait();                                               // everything below follows from what is read from here on
     const bool ranked = a.n_seqs <= PT_SORTED;
     const int per_unit = 2 * TT;
@@ -246,10 +246,12 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem;
+    // only now: a kernel that starts earlier might take the tensor memory and wait for this one
+    dep_release();
 
     // unit number n of this CTA; false once the CTA is aborting
     auto take_unit = [&](uint32_t n, PtUnit& u) {
-        if (!wait_asleep(bar(ctl.unit_full[n % PT_UNITS]), (n / PT_UNITS) & 1u, abort_flag, a.status)) return false;
+        if (!wait_asleep(bar(ctl.unit_full[n % PT_UNITS]), (n / PT_UNITS) & 1u, abort_flag, status)) return false;
         const int4* p = reinterpret_cast<const int4*>(&ctl.units[n % PT_UNITS]);
         const int4 x = p[0], y = p[1], z = SPLIT ? p[2] : make_int4(0, 0, 0, 0);
         u = PtUnit{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, {0, 0}};
@@ -292,7 +294,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             uint64_t sum0 = pk2(0.f, 0.f), sum1 = sum0;
             for (int j = 0; j < blocks; ++j, ++steps) {
                 const uint32_t buffer = steps % 2, t_s = lanes + Lay::s_col(tile, buffer);
-                ok = wait_asleep(bar(ctl.s_ready[tile][buffer]), (steps / 2) & 1u, abort_flag, a.status);
+                ok = wait_asleep(bar(ctl.s_ready[tile][buffer]), (steps / 2) & 1u, abort_flag, status);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -318,7 +320,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     m = up;
                     sum0 = mul2(sum0, pk2(f, f));
                     sum1 = mul2(sum1, pk2(f, f));
-                    ok = wait_asleep(bar(ctl.pv_done[tile]), (steps - 1) & 1u, abort_flag, a.status);
+                    ok = wait_asleep(bar(ctl.pv_done[tile]), (steps - 1) & 1u, abort_flag, status);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) break;
                     tc_fence_after();
@@ -365,7 +367,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
             if (!ok) break;
             float inv = 0.f, l = 0.f;
             if (blocks > 0) {
-                ok = wait_asleep(bar(ctl.o_ready[tile]), tiles & 1u, abort_flag, a.status);
+                ok = wait_asleep(bar(ctl.o_ready[tile]), tiles & 1u, abort_flag, status);
                 ++tiles;
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
@@ -458,7 +460,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     if (s.mine > 0) ++q_next;
                     return true;
                 };
-                auto full = [&](uint32_t at) { return wait_asleep(bar(ctl.kv_full[at % Lay::KV_SLOTS]), (at / Lay::KV_SLOTS) & 1u, abort_flag, a.status); };
+                auto full = [&](uint32_t at) { return wait_asleep(bar(ctl.kv_full[at % Lay::KV_SLOTS]), (at / Lay::KV_SLOTS) & 1u, abort_flag, status); };
                 auto scores = [&](const Step& s) {
                     const uint32_t k_slot = s.kv % Lay::KV_SLOTS;
                     if (s.j >= s.mine) {
@@ -469,7 +471,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     const uint32_t q_slot = Lay::q_slot(i, s.q), buffer = s_count++ & 1u, to = tmem + Lay::s_col(i, buffer);
                     const uint64_t dq = smem_desc(q_s((int)q_slot), 128), dk = smem_desc(kv_s((int)k_slot), 128);
                     const uint32_t idesc = s.j + 1 < s.mine ? idesc_s : instr_desc(round16(block_keys(s.u, i, s.j, TT, a.causal)));
-                    if (s.j == 0) ok = wait_asleep(bar(ctl.q_full[q_slot]), (s.q >> 1) & 1u, abort_flag, a.status);
+                    if (s.j == 0) ok = wait_asleep(bar(ctl.q_full[q_slot]), (s.q >> 1) & 1u, abort_flag, status);
                     ok = ok && full(s.kv);
                     if (!ok) return;
                     tc_fence_after();
@@ -491,7 +493,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     const uint64_t dv = v_desc<D>(kv_s((int)v_slot));
                     const int pieces = s.j + 1 < s.mine ? PT_KEYS / 16 : round16(block_keys(s.u, i, s.j, TT, a.causal)) / 16;
                     const uint32_t add = s.j > 0 ? 1u : 0u;
-                    ok = ok && wait_asleep(bar(ctl.p_ready[i][buffer]), (p_count++ >> 1) & 1u, abort_flag, a.status);
+                    ok = ok && wait_asleep(bar(ctl.p_ready[i][buffer]), (p_count++ >> 1) & 1u, abort_flag, status);
                     if (!ok) return;
                     tc_fence_after();
                     if (pieces == PT_KEYS / 16) {
@@ -617,7 +619,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     left += 2 * ((units & 1u) ? blockIdx.x : gridDim.x - 1 - blockIdx.x) + 1;
                 }
                 const int at = (int)(units % PT_UNITS);
-                ok = wait_asleep(bar(ctl.unit_empty[at]), ((units / PT_UNITS) & 1u) ^ 1u, abort_flag, a.status);
+                ok = wait_asleep(bar(ctl.unit_empty[at]), ((units / PT_UNITS) & 1u) ^ 1u, abort_flag, status);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 if (lane == 0) {
@@ -636,7 +638,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     auto load_q = [&](int i) {
                         uint32_t& use = i ? q1 : q0;
                         const int slot = (int)Lay::q_slot(i, use);
-                        ok = ok && wait_asleep(bar(ctl.q_empty[slot]), ((use >> 1) & 1u) ^ 1u, abort_flag, a.status);
+                        ok = ok && wait_asleep(bar(ctl.q_empty[slot]), ((use >> 1) & 1u) ^ 1u, abort_flag, status);
                         if (!ok) return;
                         mbar_expect_tx(bar(ctl.q_full[slot]), (uint32_t)(TT * a.group * D * 2));
                         for (int x = 0; x < D / 64; ++x)
@@ -645,7 +647,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                     };
                     auto load_kv = [&](const CUtensorMap* tm, int j, unsigned long long* full) {
                         const int slot = (int)(kv % Lay::KV_SLOTS);
-                        ok = ok && wait_asleep(bar(ctl.kv_empty[slot]), ((kv / Lay::KV_SLOTS) & 1u) ^ 1u, abort_flag, a.status);
+                        ok = ok && wait_asleep(bar(ctl.kv_empty[slot]), ((kv / Lay::KV_SLOTS) & 1u) ^ 1u, abort_flag, status);
                         if (!ok) return;
                         const uint32_t on = full ? bar(*full) : bar(ctl.kv_full[slot]);
                         mbar_expect_tx(on, (uint32_t)Lay::KV_BYTES);
@@ -681,7 +683,7 @@ attention_packed_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
                 kv += 2 * (uint32_t)blocks;
                 if (!has_tail(u)) continue;
                 const int slot = (int)((kv - 1) % Lay::KV_SLOTS);
-                ok = wait_asleep(bar(ctl.tail[tails % PT_TAILS]), (tails / PT_TAILS) & 1u, abort_flag, a.status);
+                ok = wait_asleep(bar(ctl.tail[tails % PT_TAILS]), (tails / PT_TAILS) & 1u, abort_flag, status);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 ++tails;

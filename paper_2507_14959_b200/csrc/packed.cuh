@@ -12,7 +12,7 @@ struct PackedArgs {
     int q_rows, kv_rows, n_seqs, max_q, max_kv;
     int heads, kv_heads, group, causal;
     float c;                                                 // scale * log2(e)
-    int* status;
+    int* status;                                             // or null, see packed_status
 };
 
 
@@ -22,6 +22,10 @@ size_t packed_tc_workspace(const PackedArgs& a, int head_dim, int splits);
 cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim, int n_sms, int splits, void* workspace);
 
 namespace {
+
+// Where calls without a status word of their own leave what they find.
+__device__ int packed_status_word;
+__device__ __forceinline__ int* packed_status(const PackedArgs& a) { return a.status ? a.status : &packed_status_word; }
 
 struct Segment { int q0, nq, k0, nk; };
 
@@ -35,7 +39,7 @@ __device__ __forceinline__ Segment packed_segment(const PackedArgs& a, int s) {
     const long long n_q = (long long)q1 - q0, n_k = a.kv_lengths ? (long long)length : (long long)k_next - k_at;
     const bool ok = q0 >= 0 && n_q >= 0 && q1 <= a.q_rows && n_q <= a.max_q && k_at >= 0 && n_k >= 0 && n_k <= a.max_kv && k_at + n_k <= a.kv_rows;
     if (!ok) {
-        atomicCAS(a.status, 0, (int)PM_ERR_ARG);
+        atomicCAS(packed_status(a), 0, (int)PM_ERR_ARG);
         return Segment{0, 0, 0, 0};
     }
     return Segment{q0, (int)n_q, k_at, (int)n_k};
