@@ -643,10 +643,11 @@ def _workspace(lib, args, like, stream):
         raise PolymorphError(rc, "pm_attention_packed_workspace")
     if not need.value:
         return None
-    space = torch.empty(need.value, dtype=torch.uint8, device=like.device)
-    if stream is not None:
-        space.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream)))
-    return space
+    if stream is None:
+        return torch.empty(need.value, dtype=torch.uint8, device=like.device)
+    # what torch gives out on the current stream may still be in use there when another stream gets to it
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream))):
+        return torch.empty(need.value, dtype=torch.uint8, device=like.device)
 
 
 def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offsets=None, kv_lengths=None, causal=False, scale=None, status=None,
@@ -679,7 +680,10 @@ def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offset
         sp = _indexes(where, "status", status, here, 1)
     fields = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), qs, ks, v_shape[3], o_shape[3], qo, ko, kl, rows, kv_rows, n, max_q, max_kv, heads,
               kv_heads, dim, 1 if causal else 0, 0.0 if scale is None else scale, dtype, sp)
-    args = _ATTENTION_ARGS.pack(*fields, 0, 0)
+    try:
+        args = _ATTENTION_ARGS.pack(*fields, 0, 0)
+    except struct.error as e:
+        _refuse(where, e)
     if max_kv >= LONG_HISTORY and dtype == 0 and (n * kv_heads + rows * heads // 128) <= MANY_UNITS:
         space = _workspace(lib, args, q, stream)
         if space is not None:

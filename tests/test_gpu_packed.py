@@ -399,6 +399,77 @@ def test_a_captured_call_replays_with_other_lengths_and_values(lengths):
             assert ((replayed[at:at + a].double() - want).abs() <= bound(0, want, mean, sizes, 64, b)).all()
 
 
+def test_first_calls_of_a_process_may_be_captured():
+    """Nothing is set up by a first call that a capture could not hold."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2507_14959_b200 import binding
+ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+x = torch.randn(600, 8, 64, device="cuda").bfloat16()
+table, at, g1 = binding.RopeTable(64), ints(list(range(600))), torch.ones(64, device="cuda")
+outs = [torch.zeros_like(x) for _ in range(5)]
+few, all_, hist = ints([0, 3]), ints([0, 100, 600]), ints([0, 600])
+def calls(o):
+    binding.rope(x, o[0], at, table, 0)
+    binding.qk_norm_rope(x, None, o[1], None, g1, None, norm="rms", eps=1e-6, dtype=0, positions=at, table=table)
+    binding.attention_packed(x, x, x, o[2], few, 3, 600, 0, kv_offsets=hist, causal=True)
+    binding.attention_packed(x, x, x, o[3], all_, 500, 500, 0)
+    f = x.float()
+    binding.attention_packed(f, f, f, o[4].float(), all_, 500, 500, 1)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls(outs)
+graph.replay()
+torch.cuda.synchronize()
+eager = [torch.zeros_like(x) for _ in range(5)]
+calls(eager)
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(outs, eager)) and outs[3].abs().sum() > 0
+print("captured")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "captured" in done.stdout, done.stderr[-2000:]
+
+
+def test_a_workspace_on_another_stream_than_torchs():
+    """The call's stream is given, torch's current one is busy with memory it has already given back: the workspace is none of that."""
+    from paper_2507_14959_b200 import binding
+    n, heads, kv_heads, dim = 16000, 8, 2, 128
+    q, k, v = normal(1, 1, heads, dim).bfloat16().cuda(), normal(2, n, kv_heads, dim).bfloat16().cuda(), normal(3, n, kv_heads, dim).bfloat16().cuda()
+    out, q_off, k_off, other = torch.zeros_like(q), ints([0, 1]), ints([0, n]), torch.cuda.Stream()
+    want, mean, size = expected(q, k, v, True, dim ** -0.5)
+    kept = torch.zeros(1 << 20, device="cuda")
+    torch.cuda.synchronize()
+    for turn in range(5):
+        torch.cuda._sleep(20_000_000)                      # the current stream is behind
+        lent = torch.full((1 << 20,), float(turn + 1), device="cuda")
+        kept.copy_(lent)
+        del lent                                           # its memory may be given out again on the current stream
+        binding.attention_packed(q, k, v, out, q_off, 1, n, 0, kv_offsets=k_off, causal=True, stream=other if turn % 2 else other.cuda_stream)
+        torch.cuda.synchronize()
+        assert (kept == turn + 1).all()
+        assert ((out.double() - want).abs() <= bound(0, want, mean, size, dim, n)).all()
+
+
+def test_units_that_share_their_keys():
+    """Few units over long histories: their keys are cut into parts, which a second kernel joins."""
+    from paper_2507_14959_b200 import binding
+    for dim, heads, kv_heads, lengths in ((128, 8, 2, [(256, 8000)]), (64, 4, 4, [(3000, 8192), (0, 500), (257, 0), (5, 5000)]), (64, 6, 2, [(700, 9000), (90, 300)]),
+                                          (128, 5, 5, [(4096, 4096)])):
+        for causal in (True, False):
+            form = binding.attention_packed_kernel(heads=heads, kv_heads=kv_heads, head_dim=dim, n_seqs=len(lengths), max_q=max(a for a, _ in lengths),
+                                                   max_kv=max(b for _, b in lengths), q_rows=sum(a for a, _ in lengths) + 3, kv_rows=sum(b for _, b in lengths) + 3,
+                                                   workspace_bytes=1 << 28)
+            if causal:
+                assert form[0] == "tcgen05" and form[2] > 1, form
+            check(0, dim, heads, kv_heads, lengths, causal, seed=71)
+
+
 def test_other_streams_side_by_side():
     """Calls on two streams share nothing."""
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
