@@ -465,7 +465,7 @@ typedef struct {
     const int32_t* kv_lengths;            /* dev int32 [n_seqs]: number of keys of each sequence (slots of a cache); NULL: kv_offsets[s + 1] - kv_offsets[s] */
     int q_rows, kv_rows;                  /* rows of the buffers                                               */
     int n_seqs;                           /* at most PM_PACKED_MAX_SEQS                                        */
-    int max_q, max_kv;                    /* no sequence has more queries, keys than this                      */
+    int max_q, max_kv;                    /* no sequence has more queries, keys than this (the kernel is chosen by it; far too large costs little) */
     int heads, kv_heads;                  /* heads a multiple of kv_heads, at most PM_PACKED_MAX_GROUP times   */
     int head_dim;                         /* 64 or 128                                                         */
     int causal;

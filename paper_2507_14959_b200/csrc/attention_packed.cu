@@ -7,7 +7,7 @@
 //   attention_f32_kernel    fp32 on CUDA cores
 // Both keep the running maximum m, sum l and unnormalised output O of a row in fp32 while they pass over the keys once, and join
 // the parts of a row as  m = max m_i,  l = sum l_i 2^(m_i - m),  O = sum O_i 2^(m_i - m)  through shared memory, that of the
-// cluster where the keys are split among CTAs: no workspace, no atomics, the order of every sum fixed.
+// cluster or a workspace where the keys are split among CTAs: no atomics, the order of every sum fixed.
 #include <math.h>
 
 #include <algorithm>
@@ -97,208 +97,212 @@ __global__ void __launch_bounds__(32 * ROWS_WARPS) attention_rows_kernel(const _
     extern __shared__ __align__(128) uint8_t smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, mi = lane >> 3, l7 = lane & 7;
-    const int share = cluster * splits, rank = blockIdx.x % share, tile = blockIdx.x / share;
+    const int share = cluster * splits, rank = blockIdx.x % share, in_grid = gridDim.x / share;
     const int h = blockIdx.y;
     dep_release();
     dep_wait();
     const Segment seg = packed_segment(a, blockIdx.z);
-    const int rows = seg.nq * a.group, r0 = tile * 16;
-    if (r0 >= rows) return;                                             // the whole cluster's tile
-    const int r_lo = min(r0 + g, rows - 1), r_hi = min(r0 + g + 8, rows - 1), r_last = min(r0 + 15, rows - 1);
-    const int vis_lo = packed_visible(seg, r_lo / a.group, a.causal), vis_hi = packed_visible(seg, r_hi / a.group, a.causal);
-    const int k_end = packed_visible(seg, r_last / a.group, a.causal), k_all = packed_visible(seg, r0 / a.group, a.causal);
-    // query fragments from global memory; rows past the end repeat the last one and are not stored
-    uint32_t qa[D / 16][4];
-    {
-        const bf16* lo = (const bf16*)a.q + (long long)(seg.q0 + r_lo / a.group) * a.q_stride + (h * a.group + r_lo % a.group) * D;
-        const bf16* hi = (const bf16*)a.q + (long long)(seg.q0 + r_hi / a.group) * a.q_stride + (h * a.group + r_hi % a.group) * D;
+    const int rows = seg.nq * a.group, tiles = (rows + 15) / 16;
+    for (int tile = blockIdx.x / share; tile < tiles; tile += in_grid) {  // the same for a whole cluster
+        const int r0 = tile * 16;
+        const int r_lo = min(r0 + g, rows - 1), r_hi = min(r0 + g + 8, rows - 1), r_last = min(r0 + 15, rows - 1);
+        const int vis_lo = packed_visible(seg, r_lo / a.group, a.causal), vis_hi = packed_visible(seg, r_hi / a.group, a.causal);
+        const int k_end = packed_visible(seg, r_last / a.group, a.causal), k_all = packed_visible(seg, r0 / a.group, a.causal);
+        // query fragments from global memory; rows past the end repeat the last one and are not stored
+        uint32_t qa[D / 16][4];
+        {
+            const bf16* lo = (const bf16*)a.q + (long long)(seg.q0 + r_lo / a.group) * a.q_stride + (h * a.group + r_lo % a.group) * D;
+            const bf16* hi = (const bf16*)a.q + (long long)(seg.q0 + r_hi / a.group) * a.q_stride + (h * a.group + r_hi % a.group) * D;
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-            const int c = ks * 16 + 2 * t;
-            qa[ks][0] = *reinterpret_cast<const uint32_t*>(lo + c);
-            qa[ks][1] = *reinterpret_cast<const uint32_t*>(hi + c);
-            qa[ks][2] = *reinterpret_cast<const uint32_t*>(lo + c + 8);
-            qa[ks][3] = *reinterpret_cast<const uint32_t*>(hi + c + 8);
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const int c = ks * 16 + 2 * t;
+                qa[ks][0] = *reinterpret_cast<const uint32_t*>(lo + c);
+                qa[ks][1] = *reinterpret_cast<const uint32_t*>(hi + c);
+                qa[ks][2] = *reinterpret_cast<const uint32_t*>(lo + c + 8);
+                qa[ks][3] = *reinterpret_cast<const uint32_t*>(hi + c + 8);
+            }
         }
-    }
-    const uint32_t ring = smem_u32(sm.ring[warp]);
-    const bf16* kp = (const bf16*)a.k + (long long)seg.k0 * a.k_stride + h * D;
-    const bf16* vp = (const bf16*)a.v + (long long)seg.k0 * a.v_stride + h * D;
-    const int chunks = (k_end + 15) >> 4, step = share * ROWS_WARPS;
-    auto fetch = [&](int chunk, int stage) {
-        const uint32_t ks = ring + (uint32_t)(stage * 2 * 16 * D * 2), vs = ks + 16 * D * 2;
+        const uint32_t ring = smem_u32(sm.ring[warp]);
+        const bf16* kp = (const bf16*)a.k + (long long)seg.k0 * a.k_stride + h * D;
+        const bf16* vp = (const bf16*)a.v + (long long)seg.k0 * a.v_stride + h * D;
+        const int chunks = (k_end + 15) >> 4, step = share * ROWS_WARPS;
+        auto fetch = [&](int chunk, int stage) {
+            const uint32_t ks = ring + (uint32_t)(stage * 2 * 16 * D * 2), vs = ks + 16 * D * 2;
 #pragma unroll
-        for (int i = 0; i < 16 * CH / 32; ++i) {
-            const int at = i * 32 + lane, r = at / CH, c = at % CH, key = chunk * 16 + r;
-            const bool real = key < k_end;
-            const long long row = real ? key : 0;
-            const uint32_t to = (uint32_t)(r * D * 2 + ((c ^ (r & 7)) << 4));
-            copy16(ks + to, kp + row * a.k_stride + c * 8, real);
-            copy16(vs + to, vp + row * a.v_stride + c * 8, real);
+            for (int i = 0; i < 16 * CH / 32; ++i) {
+                const int at = i * 32 + lane, r = at / CH, c = at % CH, key = chunk * 16 + r;
+                const bool real = key < k_end;
+                const long long row = real ? key : 0;
+                const uint32_t to = (uint32_t)(r * D * 2 + ((c ^ (r & 7)) << 4));
+                copy16(ks + to, kp + row * a.k_stride + c * 8, real);
+                copy16(vs + to, vp + row * a.v_stride + c * 8, real);
+            }
+        };
+        float o[D / 8][4], m_lo = -INFINITY, m_hi = -INFINITY, l_lo = 0.f, l_hi = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        const int first = rank * ROWS_WARPS + warp;
+#pragma unroll
+        for (int i = 0; i < ROWS_STAGES - 1; ++i) {
+            if (first + i * step < chunks) fetch(first + i * step, i);
+            copy_commit();
         }
-    };
-    float o[D / 8][4], m_lo = -INFINITY, m_hi = -INFINITY, l_lo = 0.f, l_hi = 0.f;
+        int stage = 0;
+        for (int chunk = first; chunk < chunks; chunk += step) {
+            const int ahead = chunk + (ROWS_STAGES - 1) * step, ahead_stage = stage == 0 ? ROWS_STAGES - 1 : stage - 1;
+            if (ahead < chunks) fetch(ahead, ahead_stage);                  // the stage read one step ago
+            copy_commit();
+            copy_wait<ROWS_STAGES - 1>();
+            __syncwarp();
+            const uint32_t ks_at = ring + (uint32_t)(stage * 2 * 16 * D * 2), vs_at = ks_at + 16 * D * 2;
+            float s[2][4] = {};
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    const int first = rank * ROWS_WARPS + warp;
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const int r = (mi >> 1) * 8 + l7, c = ks * 2 + (mi & 1);
+                uint32_t b[4];
+                ldsm4(ks_at + r * D * 2 + ((c ^ (r & 7)) << 4), b);
+                mma16816(s[0], qa[ks], b[0], b[1]);
+                mma16816(s[1], qa[ks], b[2], b[3]);
+            }
+            const bool whole = chunk * 16 + 16 <= k_all;
+            float b_lo = m_lo, b_hi = m_hi;
 #pragma unroll
-    for (int i = 0; i < ROWS_STAGES - 1; ++i) {
-        if (first + i * step < chunks) fetch(first + i * step, i);
-        copy_commit();
-    }
-    int stage = 0;
-    for (int chunk = first; chunk < chunks; chunk += step) {
-        const int ahead = chunk + (ROWS_STAGES - 1) * step, ahead_stage = stage == 0 ? ROWS_STAGES - 1 : stage - 1;
-        if (ahead < chunks) fetch(ahead, ahead_stage);                  // the stage read one step ago
-        copy_commit();
-        copy_wait<ROWS_STAGES - 1>();
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = chunk * 16 + i * 8 + 2 * t + (e & 1);
+                    const float x = s[i][e] * a.c;
+                    s[i][e] = whole || key < (e < 2 ? vis_lo : vis_hi) ? x : -INFINITY;
+                    if (e < 2) b_lo = fmaxf(b_lo, s[i][e]);
+                    else b_hi = fmaxf(b_hi, s[i][e]);
+                }
+            b_lo = fmaxf(b_lo, __shfl_xor_sync(0xFFFFFFFFu, b_lo, 1));
+            b_lo = fmaxf(b_lo, __shfl_xor_sync(0xFFFFFFFFu, b_lo, 2));
+            b_hi = fmaxf(b_hi, __shfl_xor_sync(0xFFFFFFFFu, b_hi, 1));
+            b_hi = fmaxf(b_hi, __shfl_xor_sync(0xFFFFFFFFu, b_hi, 2));
+            if (__any_sync(0xFFFFFFFFu, b_lo > m_lo || b_hi > m_hi)) {      // a larger maximum: what is there is taken down to it
+                const float f_lo = b_lo == m_lo ? 1.f : ex2(m_lo - b_lo), f_hi = b_hi == m_hi ? 1.f : ex2(m_hi - b_hi);
+                m_lo = b_lo; m_hi = b_hi;
+                l_lo *= f_lo; l_hi *= f_hi;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) { o[i][0] *= f_lo; o[i][1] *= f_lo; o[i][2] *= f_hi; o[i][3] *= f_hi; }
+            }
+            // a row that has seen nothing yet keeps -inf and adds nothing
+            const float n_lo = m_lo == -INFINITY ? 0.f : m_lo, n_hi = m_hi == -INFINITY ? 0.f : m_hi;
+            uint32_t pa[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float p0 = ex2(s[i][0] - n_lo), p1 = ex2(s[i][1] - n_lo), p2 = ex2(s[i][2] - n_hi), p3 = ex2(s[i][3] - n_hi);
+                l_lo += p0 + p1;
+                l_hi += p2 + p3;
+                pa[i * 2] = pack(p0, p1);
+                pa[i * 2 + 1] = pack(p2, p3);
+            }
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) {
+                const int r = (mi & 1) * 8 + l7, c = n * 2 + (mi >> 1);
+                uint32_t b[4];
+                ldsm4_t(vs_at + r * D * 2 + ((c ^ (r & 7)) << 4), b);
+                mma16816(o[2 * n], pa, b[0], b[1]);
+                mma16816(o[2 * n + 1], pa, b[2], b[3]);
+            }
+            __syncwarp();                                                   // this stage is fetched into again at the next step
+            stage = stage == ROWS_STAGES - 1 ? 0 : stage + 1;
+        }
+        copy_wait<0>();
         __syncwarp();
-        const uint32_t ks_at = ring + (uint32_t)(stage * 2 * 16 * D * 2), vs_at = ks_at + 16 * D * 2;
-        float s[2][4] = {};
+        l_lo += __shfl_xor_sync(0xFFFFFFFFu, l_lo, 1);
+        l_lo += __shfl_xor_sync(0xFFFFFFFFu, l_lo, 2);
+        l_hi += __shfl_xor_sync(0xFFFFFFFFu, l_hi, 1);
+        l_hi += __shfl_xor_sync(0xFFFFFFFFu, l_hi, 2);
+        float* part = reinterpret_cast<float*>(sm.ring[warp]);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-            const int r = (mi >> 1) * 8 + l7, c = ks * 2 + (mi & 1);
-            uint32_t b[4];
-            ldsm4(ks_at + r * D * 2 + ((c ^ (r & 7)) << 4), b);
-            mma16816(s[0], qa[ks], b[0], b[1]);
-            mma16816(s[1], qa[ks], b[2], b[3]);
+        for (int i = 0; i < D / 8; ++i) {
+            *reinterpret_cast<float2*>(part + g * Smem::PART + i * 8 + 2 * t) = make_float2(o[i][0], o[i][1]);
+            *reinterpret_cast<float2*>(part + (g + 8) * Smem::PART + i * 8 + 2 * t) = make_float2(o[i][2], o[i][3]);
         }
-        const bool whole = chunk * 16 + 16 <= k_all;
-        float b_lo = m_lo, b_hi = m_hi;
+        if (t == 0) {
+            sm.m[warp][g] = m_lo; sm.l[warp][g] = l_lo;
+            sm.m[warp][g + 8] = m_hi; sm.l[warp][g + 8] = l_hi;
+        }
+        __syncthreads();
+        // the warps' parts: eight threads a row
+        {
+            constexpr int EACH = D / 8;
+            const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;   // columns c0 .. c0 + 3 of every 32
+            float m = sm.m[0][row];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int w = 1; w < ROWS_WARPS; ++w) m = fmaxf(m, sm.m[w][row]);
+            const float base = m == -INFINITY ? 0.f : m;
+            float l = 0.f, acc[EACH];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int key = chunk * 16 + i * 8 + 2 * t + (e & 1);
-                const float x = s[i][e] * a.c;
-                s[i][e] = whole || key < (e < 2 ? vis_lo : vis_hi) ? x : -INFINITY;
-                if (e < 2) b_lo = fmaxf(b_lo, s[i][e]);
-                else b_hi = fmaxf(b_hi, s[i][e]);
+            for (int e = 0; e < EACH; ++e) acc[e] = 0.f;
+#pragma unroll
+            for (int w = 0; w < ROWS_WARPS; ++w) {
+                const float f = ex2(sm.m[w][row] - base);                   // 0 for a warp that has seen nothing
+                l = fmaf(sm.l[w][row], f, l);
+                const float* p = reinterpret_cast<const float*>(sm.ring[w]) + row * Smem::PART + c0;
+#pragma unroll
+                for (int e = 0; e < EACH; e += 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(p + e * 8);
+                    acc[e] = fmaf(x.x, f, acc[e]); acc[e + 1] = fmaf(x.y, f, acc[e + 1]);
+                    acc[e + 2] = fmaf(x.z, f, acc[e + 2]); acc[e + 3] = fmaf(x.w, f, acc[e + 3]);
+                }
             }
-        b_lo = fmaxf(b_lo, __shfl_xor_sync(0xFFFFFFFFu, b_lo, 1));
-        b_lo = fmaxf(b_lo, __shfl_xor_sync(0xFFFFFFFFu, b_lo, 2));
-        b_hi = fmaxf(b_hi, __shfl_xor_sync(0xFFFFFFFFu, b_hi, 1));
-        b_hi = fmaxf(b_hi, __shfl_xor_sync(0xFFFFFFFFu, b_hi, 2));
-        if (__any_sync(0xFFFFFFFFu, b_lo > m_lo || b_hi > m_hi)) {      // a larger maximum: what is there is taken down to it
-            const float f_lo = b_lo == m_lo ? 1.f : ex2(m_lo - b_lo), f_hi = b_hi == m_hi ? 1.f : ex2(m_hi - b_hi);
-            m_lo = b_lo; m_hi = b_hi;
-            l_lo *= f_lo; l_hi *= f_hi;
+            if (splits > 1) {
+                RowsPart<D>& part = parts[((size_t)(blockIdx.z * a.kv_heads + h) * in_grid + tile) * splits + rank];
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) { o[i][0] *= f_lo; o[i][1] *= f_lo; o[i][2] *= f_hi; o[i][3] *= f_hi; }
-        }
-        // a row that has seen nothing yet keeps -inf and adds nothing
-        const float n_lo = m_lo == -INFINITY ? 0.f : m_lo, n_hi = m_hi == -INFINITY ? 0.f : m_hi;
-        uint32_t pa[4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float p0 = ex2(s[i][0] - n_lo), p1 = ex2(s[i][1] - n_lo), p2 = ex2(s[i][2] - n_hi), p3 = ex2(s[i][3] - n_hi);
-            l_lo += p0 + p1;
-            l_hi += p2 + p3;
-            pa[i * 2] = pack(p0, p1);
-            pa[i * 2 + 1] = pack(p2, p3);
-        }
-#pragma unroll
-        for (int n = 0; n < D / 16; ++n) {
-            const int r = (mi & 1) * 8 + l7, c = n * 2 + (mi >> 1);
-            uint32_t b[4];
-            ldsm4_t(vs_at + r * D * 2 + ((c ^ (r & 7)) << 4), b);
-            mma16816(o[2 * n], pa, b[0], b[1]);
-            mma16816(o[2 * n + 1], pa, b[2], b[3]);
-        }
-        __syncwarp();                                                   // this stage is fetched into again at the next step
-        stage = stage == ROWS_STAGES - 1 ? 0 : stage + 1;
-    }
-    copy_wait<0>();
-    __syncwarp();
-    l_lo += __shfl_xor_sync(0xFFFFFFFFu, l_lo, 1);
-    l_lo += __shfl_xor_sync(0xFFFFFFFFu, l_lo, 2);
-    l_hi += __shfl_xor_sync(0xFFFFFFFFu, l_hi, 1);
-    l_hi += __shfl_xor_sync(0xFFFFFFFFu, l_hi, 2);
-    float* part = reinterpret_cast<float*>(sm.ring[warp]);
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-        *reinterpret_cast<float2*>(part + g * Smem::PART + i * 8 + 2 * t) = make_float2(o[i][0], o[i][1]);
-        *reinterpret_cast<float2*>(part + (g + 8) * Smem::PART + i * 8 + 2 * t) = make_float2(o[i][2], o[i][3]);
-    }
-    if (t == 0) {
-        sm.m[warp][g] = m_lo; sm.l[warp][g] = l_lo;
-        sm.m[warp][g + 8] = m_hi; sm.l[warp][g + 8] = l_hi;
-    }
-    __syncthreads();
-    // the warps' parts: eight threads a row
-    {
-        constexpr int EACH = D / 8;
-        const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;   // columns c0 .. c0 + 3 of every 32
-        float m = sm.m[0][row];
-#pragma unroll
-        for (int w = 1; w < ROWS_WARPS; ++w) m = fmaxf(m, sm.m[w][row]);
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f, acc[EACH];
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) acc[e] = 0.f;
-#pragma unroll
-        for (int w = 0; w < ROWS_WARPS; ++w) {
-            const float f = ex2(sm.m[w][row] - base);                   // 0 for a warp that has seen nothing
-            l = fmaf(sm.l[w][row], f, l);
-            const float* p = reinterpret_cast<const float*>(sm.ring[w]) + row * Smem::PART + c0;
-#pragma unroll
-            for (int e = 0; e < EACH; e += 4) {
-                const float4 x = *reinterpret_cast<const float4*>(p + e * 8);
-                acc[e] = fmaf(x.x, f, acc[e]); acc[e + 1] = fmaf(x.y, f, acc[e + 1]);
-                acc[e + 2] = fmaf(x.z, f, acc[e + 2]); acc[e + 3] = fmaf(x.w, f, acc[e + 3]);
+                for (int e = 0; e < EACH; e += 4) *reinterpret_cast<float4*>(&part.o[row][c0 + e * 8]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+                if ((threadIdx.x & 7) == 0) { part.m[row] = m; part.l[row] = l; }
+                return;                                                     // all tiles are in the grid
             }
-        }
-        if (splits > 1) {
-            RowsPart<D>& part = parts[((size_t)(blockIdx.z * a.kv_heads + h) * (gridDim.x / splits) + tile) * splits + rank];
+            if (cluster == 1) {
+                const int r = r0 + row;
+                if (r < rows) {
+                    const float inv = l == 0.f ? 0.f : 1.f / l;
+                    bf16* to = (bf16*)a.out + (long long)(seg.q0 + r / a.group) * a.out_stride + (h * a.group + r % a.group) * D + c0;
 #pragma unroll
-            for (int e = 0; e < EACH; e += 4) *reinterpret_cast<float4*>(&part.o[row][c0 + e * 8]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
-            if ((threadIdx.x & 7) == 0) { part.m[row] = m; part.l[row] = l; }
-            return;
-        }
-        if (cluster == 1) {
-            const int r = r0 + row;
-            if (r < rows) {
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                bf16* to = (bf16*)a.out + (long long)(seg.q0 + r / a.group) * a.out_stride + (h * a.group + r % a.group) * D + c0;
-#pragma unroll
-                for (int e = 0; e < EACH; e += 4)
-                    *reinterpret_cast<uint2*>(to + e * 8) = make_uint2(pack(acc[e] * inv, acc[e + 1] * inv), pack(acc[e + 2] * inv, acc[e + 3] * inv));
+                    for (int e = 0; e < EACH; e += 4)
+                        *reinterpret_cast<uint2*>(to + e * 8) = make_uint2(pack(acc[e] * inv, acc[e + 1] * inv), pack(acc[e + 2] * inv, acc[e + 3] * inv));
+                }
+                if (tile + in_grid >= tiles) return;
+                __syncthreads();                                            // the next tile's keys land on the parts
+                continue;
             }
-            return;
-        }
 #pragma unroll
-        for (int e = 0; e < EACH; e += 4) *reinterpret_cast<float4*>(&sm.o_cta[row][c0 + e * 8]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
-        if ((threadIdx.x & 7) == 0) { sm.m_cta[row] = m; sm.l_cta[row] = l; }
+            for (int e = 0; e < EACH; e += 4) *reinterpret_cast<float4*>(&sm.o_cta[row][c0 + e * 8]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+            if ((threadIdx.x & 7) == 0) { sm.m_cta[row] = m; sm.l_cta[row] = l; }
+        }
+        cluster_sync_all();
+        // the CTAs' parts: each CTA joins 16 / cluster rows, a pair of columns per thread and turn
+        const int mine = 16 / cluster;
+        for (int i = threadIdx.x; i < mine * D / 2; i += 32 * ROWS_WARPS) {
+            const int row = rank * mine + i / (D / 2), col = i % (D / 2) * 2, r = r0 + row;
+            if (r >= rows) continue;
+            float ms[ROWS_MAX_CLUSTER], m = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < ROWS_MAX_CLUSTER; ++k)
+                if (k < cluster) {
+                    ms[k] = ld_cluster(mapa_cluster(smem_u32(&sm.m_cta[row]), k));
+                    m = fmaxf(m, ms[k]);
+                }
+            const float base = m == -INFINITY ? 0.f : m;
+            float l = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+            for (int k = 0; k < ROWS_MAX_CLUSTER; ++k)
+                if (k < cluster) {
+                    const float f = ex2(ms[k] - base);
+                    const float2 v = ld_cluster2(mapa_cluster(smem_u32(&sm.o_cta[row][col]), k));
+                    l = fmaf(ld_cluster(mapa_cluster(smem_u32(&sm.l_cta[row]), k)), f, l);
+                    x = fmaf(v.x, f, x);
+                    y = fmaf(v.y, f, y);
+                }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            *reinterpret_cast<uint32_t*>((bf16*)a.out + (long long)(seg.q0 + r / a.group) * a.out_stride + (h * a.group + r % a.group) * D + col) =
+                pack(x * inv, y * inv);
+        }
+        cluster_sync_all();                                                 // nobody leaves, or goes on, while its part is read
     }
-    cluster_sync_all();
-    // the CTAs' parts: each CTA joins 16 / cluster rows, a pair of columns per thread and turn
-    const int mine = 16 / cluster;
-    for (int i = threadIdx.x; i < mine * D / 2; i += 32 * ROWS_WARPS) {
-        const int row = rank * mine + i / (D / 2), col = i % (D / 2) * 2, r = r0 + row;
-        if (r >= rows) continue;
-        float ms[ROWS_MAX_CLUSTER], m = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < ROWS_MAX_CLUSTER; ++k)
-            if (k < cluster) {
-                ms[k] = ld_cluster(mapa_cluster(smem_u32(&sm.m_cta[row]), k));
-                m = fmaxf(m, ms[k]);
-            }
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f, x = 0.f, y = 0.f;
-#pragma unroll
-        for (int k = 0; k < ROWS_MAX_CLUSTER; ++k)
-            if (k < cluster) {
-                const float f = ex2(ms[k] - base);
-                const float2 v = ld_cluster2(mapa_cluster(smem_u32(&sm.o_cta[row][col]), k));
-                l = fmaf(ld_cluster(mapa_cluster(smem_u32(&sm.l_cta[row]), k)), f, l);
-                x = fmaf(v.x, f, x);
-                y = fmaf(v.y, f, y);
-            }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        *reinterpret_cast<uint32_t*>((bf16*)a.out + (long long)(seg.q0 + r / a.group) * a.out_stride + (h * a.group + r % a.group) * D + col) =
-            pack(x * inv, y * inv);
-    }
-    cluster_sync_all();                                                 // nobody leaves while its part is read
 }
 
 // Joins the splits of a row: a CTA per row, the splits in turn over its warps, lanes over the columns (one warp per row took 6 us for 74
@@ -373,173 +377,176 @@ __global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_cons
     static_assert(R * (F32_KEYS + 4) <= F32_KEYS * (D + 4), "P fits the keys");
     float (*ps)[F32_KEYS + 4] = reinterpret_cast<float (*)[F32_KEYS + 4]>(&sm.k[0][0]);
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int rank = cluster > 1 ? blockIdx.x % cluster : 0, tile = cluster > 1 ? blockIdx.x / cluster : blockIdx.x;
-    const int h = blockIdx.y;
+    const int rank = blockIdx.x % cluster, in_grid = gridDim.x / cluster, h = blockIdx.y;
     dep_release();
     dep_wait();
     const Segment seg = packed_segment(a, blockIdx.z);
-    const int rows = seg.nq * a.group, r0 = tile * R;
-    if (r0 >= rows) return;
-    const int k_end = packed_visible(seg, min(r0 + R - 1, rows - 1) / a.group, a.causal);
-    for (int i = threadIdx.x; i < R * D / 4; i += 256) {
-        const int r = i / (D / 4), c = i % (D / 4) * 4, row = r0 + r;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (row < rows)
-            x = *reinterpret_cast<const float4*>((const float*)a.q + (long long)(seg.q0 + row / a.group) * a.q_stride + (h * a.group + row % a.group) * D + c);
-        *reinterpret_cast<float4*>(&sm.q[r][c]) = x;
-    }
-    int vis[RT];
-    float m[RT], l[RT];
-    uint64_t o[RT][DT][2];                                              // four columns, packed
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        vis[i] = packed_visible(seg, min(r0 + ty + 16 * i, rows - 1) / a.group, a.causal);
-        m[i] = -INFINITY; l[i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < DT; ++j) o[i][j][0] = o[i][j][1] = 0ull;
-    }
-    // a warp (two thread rows) without a real row in it only helps to copy; the warp as a whole, for its shuffles
-    const bool active = R > 16 || r0 + (ty & ~1) < rows;
-    const float* kp = (const float*)a.k + (long long)seg.k0 * a.k_stride + h * D;
-    const float* vp = (const float*)a.v + (long long)seg.k0 * a.v_stride + h * D;
-    for (int b0 = rank * F32_KEYS; b0 < k_end; b0 += cluster * F32_KEYS) {
-        __syncthreads();                                                // the block before has been read
-        for (int i = threadIdx.x; i < F32_KEYS * D / 4; i += 256) {
-            const int r = i / (D / 4), c = i % (D / 4) * 4, key = b0 + r;
-            const bool real = key < k_end;
-            const long long row = real ? key : 0;
-            copy16(smem_u32(&sm.k[r][c]), kp + row * a.k_stride + c, real);
-            copy16(smem_u32(&sm.v[r][c]), vp + row * a.v_stride + c, real);
+    const int rows = seg.nq * a.group, tiles = (rows + R - 1) / R;
+    for (int tile = blockIdx.x / cluster; tile < tiles; tile += in_grid) {
+        const int r0 = tile * R;
+        const int k_end = packed_visible(seg, min(r0 + R - 1, rows - 1) / a.group, a.causal);
+        for (int i = threadIdx.x; i < R * D / 4; i += 256) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4, row = r0 + r;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row < rows)
+                x = *reinterpret_cast<const float4*>((const float*)a.q + (long long)(seg.q0 + row / a.group) * a.q_stride + (h * a.group + row % a.group) * D + c);
+            *reinterpret_cast<float4*>(&sm.q[r][c]) = x;
         }
-        copy_commit();
-        copy_wait<0>();
-        __syncthreads();
-        float s[RT][4];
-        if (active) {
-            uint64_t s2[RT][4];                                         // sums of the even and of the odd dimensions
+        int vis[RT];
+        float m[RT], l[RT];
+        uint64_t o[RT][DT][2];                                              // four columns, packed
 #pragma unroll
-            for (int i = 0; i < RT; ++i) s2[i][0] = s2[i][1] = s2[i][2] = s2[i][3] = 0ull;
+        for (int i = 0; i < RT; ++i) {
+            vis[i] = packed_visible(seg, min(r0 + ty + 16 * i, rows - 1) / a.group, a.causal);
+            m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < DT; ++j) o[i][j][0] = o[i][j][1] = 0ull;
+        }
+        // a warp (two thread rows) without a real row in it only helps to copy; the warp as a whole, for its shuffles
+        const bool active = R > 16 || r0 + (ty & ~1) < rows;
+        const float* kp = (const float*)a.k + (long long)seg.k0 * a.k_stride + h * D;
+        const float* vp = (const float*)a.v + (long long)seg.k0 * a.v_stride + h * D;
+        for (int b0 = rank * F32_KEYS; b0 < k_end; b0 += cluster * F32_KEYS) {
+            __syncthreads();                                                // the block before has been read
+            for (int i = threadIdx.x; i < F32_KEYS * D / 4; i += 256) {
+                const int r = i / (D / 4), c = i % (D / 4) * 4, key = b0 + r;
+                const bool real = key < k_end;
+                const long long row = real ? key : 0;
+                copy16(smem_u32(&sm.k[r][c]), kp + row * a.k_stride + c, real);
+                copy16(smem_u32(&sm.v[r][c]), vp + row * a.v_stride + c, real);
+            }
+            copy_commit();
+            copy_wait<0>();
+            __syncthreads();
+            float s[RT][4];
+            if (active) {
+                uint64_t s2[RT][4];                                         // sums of the even and of the odd dimensions
+#pragma unroll
+                for (int i = 0; i < RT; ++i) s2[i][0] = s2[i][1] = s2[i][2] = s2[i][3] = 0ull;
 #pragma unroll 4
-            for (int d = 0; d < D; d += 4) {
-                ulonglong2 q[RT], k[4];
+                for (int d = 0; d < D; d += 4) {
+                    ulonglong2 q[RT], k[4];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) q[i] = *reinterpret_cast<const ulonglong2*>(&sm.q[ty + 16 * i][d]);
+                    for (int i = 0; i < RT; ++i) q[i] = *reinterpret_cast<const ulonglong2*>(&sm.q[ty + 16 * i][d]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const ulonglong2*>(&sm.k[tx + 16 * j][d]);
+                    for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const ulonglong2*>(&sm.k[tx + 16 * j][d]);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s2[i][j] = fma2(q[i].y, k[j].y, fma2(q[i].x, k[j].x, s2[i][j]));
+                }
 #pragma unroll
                 for (int i = 0; i < RT; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s2[i][j] = fma2(q[i].y, k[j].y, fma2(q[i].x, k[j].x, s2[i][j]));
+                    for (int j = 0; j < 4; ++j) {
+                        float a0, a1;
+                        upk2(s2[i][j], a0, a1);
+                        s[i][j] = a0 + a1;
+                    }
             }
+            __syncthreads();                                                // P goes where the keys were
+            if (active) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+                for (int i = 0; i < RT; ++i) {
+                    float bm = m[i];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float a0, a1;
-                    upk2(s2[i][j], a0, a1);
-                    s[i][j] = a0 + a1;
-                }
-        }
-        __syncthreads();                                                // P goes where the keys were
-        if (active) {
-#pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                float bm = m[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[i][j] = b0 + tx + 16 * j < vis[i] ? s[i][j] * a.c : -INFINITY;
-                    bm = fmaxf(bm, s[i][j]);
-                }
-#pragma unroll
-                for (int x = 1; x < 16; x <<= 1) bm = fmaxf(bm, __shfl_xor_sync(0xFFFFFFFFu, bm, x, 16));
-                const float f = bm == m[i] ? 1.f : exp2f(m[i] - bm), base = bm == -INFINITY ? 0.f : bm;
-                m[i] = bm;
-                l[i] *= f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float p = exp2f(s[i][j] - base);
-                    l[i] += p;
-                    ps[ty + 16 * i][tx + 16 * j] = p;
-                }
-#pragma unroll
-                for (int j = 0; j < DT; ++j) { o[i][j][0] = mul2(o[i][j][0], pk2(f, f)); o[i][j][1] = mul2(o[i][j][1], pk2(f, f)); }
-            }
-        }
-        __syncthreads();
-        if (active) {
-#pragma unroll 2
-            for (int t = 0; t < F32_KEYS; t += 4) {
-                float4 p[RT];
-#pragma unroll
-                for (int i = 0; i < RT; ++i) p[i] = *reinterpret_cast<const float4*>(&ps[ty + 16 * i][t]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint64_t w[RT];
-#pragma unroll
-                    for (int i = 0; i < RT; ++i) {
-                        const float x = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
-                        w[i] = pk2(x, x);
+                    for (int j = 0; j < 4; ++j) {
+                        s[i][j] = b0 + tx + 16 * j < vis[i] ? s[i][j] * a.c : -INFINITY;
+                        bm = fmaxf(bm, s[i][j]);
                     }
 #pragma unroll
-                    for (int j = 0; j < DT; ++j) {
-                        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&sm.v[t + e][4 * tx + 64 * j]);
+                    for (int x = 1; x < 16; x <<= 1) bm = fmaxf(bm, __shfl_xor_sync(0xFFFFFFFFu, bm, x, 16));
+                    const float f = bm == m[i] ? 1.f : exp2f(m[i] - bm), base = bm == -INFINITY ? 0.f : bm;
+                    m[i] = bm;
+                    l[i] *= f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float p = exp2f(s[i][j] - base);
+                        l[i] += p;
+                        ps[ty + 16 * i][tx + 16 * j] = p;
+                    }
+#pragma unroll
+                    for (int j = 0; j < DT; ++j) { o[i][j][0] = mul2(o[i][j][0], pk2(f, f)); o[i][j][1] = mul2(o[i][j][1], pk2(f, f)); }
+                }
+            }
+            __syncthreads();
+            if (active) {
+#pragma unroll 2
+                for (int t = 0; t < F32_KEYS; t += 4) {
+                    float4 p[RT];
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) p[i] = *reinterpret_cast<const float4*>(&ps[ty + 16 * i][t]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint64_t w[RT];
 #pragma unroll
                         for (int i = 0; i < RT; ++i) {
-                            o[i][j][0] = fma2(w[i], v.x, o[i][j][0]);
-                            o[i][j][1] = fma2(w[i], v.y, o[i][j][1]);
+                            const float x = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
+                            w[i] = pk2(x, x);
+                        }
+#pragma unroll
+                        for (int j = 0; j < DT; ++j) {
+                            const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&sm.v[t + e][4 * tx + 64 * j]);
+#pragma unroll
+                            for (int i = 0; i < RT; ++i) {
+                                o[i][j][0] = fma2(w[i], v.x, o[i][j][0]);
+                                o[i][j][1] = fma2(w[i], v.y, o[i][j][1]);
+                            }
                         }
                     }
                 }
             }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], x, 16);
-    auto address = [&](int row, int col) {
-        return (float*)a.out + (long long)(seg.q0 + row / a.group) * a.out_stride + (h * a.group + row % a.group) * D + col;
-    };
-    if (cluster == 1) {
+            for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], x, 16);
+        auto address = [&](int row, int col) {
+            return (float*)a.out + (long long)(seg.q0 + row / a.group) * a.out_stride + (h * a.group + row % a.group) * D + col;
+        };
+        if (cluster == 1) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const int row = r0 + ty + 16 * i;
+                const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+                if (row < rows)
+#pragma unroll
+                    for (int j = 0; j < DT; ++j)
+                        *reinterpret_cast<ulonglong2*>(address(row, 4 * tx + 64 * j)) = make_ulonglong2(mul2(o[i][j][0], pk2(inv, inv)), mul2(o[i][j][1], pk2(inv, inv)));
+            }
+            if (tile + in_grid >= tiles) return;
+            __syncthreads();                                                // the next tile's queries take the place of these
+            continue;
+        }
+        // parts: O where the queries were
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const int row = r0 + ty + 16 * i;
-            const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-            if (row < rows)
 #pragma unroll
-                for (int j = 0; j < DT; ++j)
-                    *reinterpret_cast<ulonglong2*>(address(row, 4 * tx + 64 * j)) = make_ulonglong2(mul2(o[i][j][0], pk2(inv, inv)), mul2(o[i][j][1], pk2(inv, inv)));
+            for (int j = 0; j < DT; ++j) *reinterpret_cast<ulonglong2*>(&sm.q[ty + 16 * i][4 * tx + 64 * j]) = make_ulonglong2(o[i][j][0], o[i][j][1]);
+            if (tx == 0) { sm.m[ty + 16 * i] = m[i]; sm.l[ty + 16 * i] = l[i]; }
         }
-        return;
-    }
-    // parts: O where the queries were
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-#pragma unroll
-        for (int j = 0; j < DT; ++j) *reinterpret_cast<ulonglong2*>(&sm.q[ty + 16 * i][4 * tx + 64 * j]) = make_ulonglong2(o[i][j][0], o[i][j][1]);
-        if (tx == 0) { sm.m[ty + 16 * i] = m[i]; sm.l[ty + 16 * i] = l[i]; }
-    }
-    cluster_sync_all();
-    const int mine = R / cluster;
-    for (int i = threadIdx.x; i < mine * D / 2; i += 256) {
-        const int row = rank * mine + i / (D / 2), col = i % (D / 2) * 2;
-        if (r0 + row >= rows) continue;
-        float top = -INFINITY;
-        for (int k = 0; k < cluster; ++k) top = fmaxf(top, ld_cluster(mapa_cluster(smem_u32(&sm.m[row]), k)));
-        const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f, x = 0.f, y = 0.f;
-        for (int k = 0; k < cluster; ++k) {
-            const float f = exp2f(ld_cluster(mapa_cluster(smem_u32(&sm.m[row]), k)) - base);
-            const float2 v = ld_cluster2(mapa_cluster(smem_u32(&sm.q[row][col]), k));
-            sum = fmaf(ld_cluster(mapa_cluster(smem_u32(&sm.l[row]), k)), f, sum);
-            x = fmaf(v.x, f, x);
-            y = fmaf(v.y, f, y);
+        cluster_sync_all();
+        const int mine = R / cluster;
+        for (int i = threadIdx.x; i < mine * D / 2; i += 256) {
+            const int row = rank * mine + i / (D / 2), col = i % (D / 2) * 2;
+            if (r0 + row >= rows) continue;
+            float top = -INFINITY;
+            for (int k = 0; k < cluster; ++k) top = fmaxf(top, ld_cluster(mapa_cluster(smem_u32(&sm.m[row]), k)));
+            const float base = top == -INFINITY ? 0.f : top;
+            float sum = 0.f, x = 0.f, y = 0.f;
+            for (int k = 0; k < cluster; ++k) {
+                const float f = exp2f(ld_cluster(mapa_cluster(smem_u32(&sm.m[row]), k)) - base);
+                const float2 v = ld_cluster2(mapa_cluster(smem_u32(&sm.q[row][col]), k));
+                sum = fmaf(ld_cluster(mapa_cluster(smem_u32(&sm.l[row]), k)), f, sum);
+                x = fmaf(v.x, f, x);
+                y = fmaf(v.y, f, y);
+            }
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            *reinterpret_cast<float2*>(address(r0 + row, col)) = make_float2(x * inv, y * inv);
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        *reinterpret_cast<float2*>(address(r0 + row, col)) = make_float2(x * inv, y * inv);
+        cluster_sync_all();
     }
-    cluster_sync_all();
 }
 
 // CTAs that share the keys of a row tile: while the grid leaves room for them and each still has `least` keys; and of long histories, whose
@@ -554,26 +561,39 @@ int key_split(long long ctas, long long slots, int max_kv, int least, int even) 
     return c;
 }
 
+// Row tiles that a call has: as many as the longest sequence may have for each, or those that the rows of the buffer can fill.
+long long tiles_of(const PackedArgs& a, int tiles, int rows) {
+    return std::min((long long)tiles * a.n_seqs, (long long)a.q_rows * a.group / rows + a.n_seqs);
+}
+// Tiles per sequence in the grid.  A CTA without a tile costs 1 ns, so with a limit far above the lengths (max_q = all rows, say) the empty
+// ones would take the time.  So no more than four times the CTAs that the rows can fill, or 16384; a longer sequence's CTAs take several
+// tiles in turn (512 frames of 197 tokens, 12 heads of 64, fp32, max_q 100864: 16.2 -> 3.0 ms, 2.9 with max_q 197).
+int tiles_in_grid(const PackedArgs& a, int tiles, int rows, int share) {
+    const long long each = std::max(4 * tiles_of(a, tiles, rows) / a.n_seqs, 16384ll / ((long long)share * a.kv_heads * a.n_seqs));
+    return (int)std::min((long long)tiles, std::max(each, 1ll));
+}
+
 // How the keys of a row tile are shared: a cluster joins in shared memory, up to eight CTAs; where even those leave most of the GPU idle and
 // there is a workspace, any number of CTAs leave their parts there and a second kernel joins them.
 struct RowsForm { int tiles, cluster, splits; };
 RowsForm rows_form(const PackedArgs& a, int n_sms, bool workspace) {
     const int tiles = (int)(((long long)a.max_q * a.group + 15) / 16);
-    const long long ctas = (long long)tiles * a.kv_heads * a.n_seqs, slots = 2ll * n_sms;
+    const long long ctas = tiles_of(a, tiles, 16) * a.kv_heads, slots = 2ll * n_sms;
     RowsForm f = {tiles, key_split(ctas, slots, a.max_kv, 16 * ROWS_WARPS, ROWS_EVEN_KEYS), 1};
     if (workspace && f.cluster == ROWS_MAX_CLUSTER && ctas * f.cluster * 2 <= slots) {
         const long long splits = std::min(slots / ctas, (long long)a.max_kv / (ROWS_SPLIT_KEYS * ROWS_WARPS));
-        if (splits >= 2 * ROWS_MAX_CLUSTER) f = {tiles, 1, (int)splits};
+        if (splits >= 2 * ROWS_MAX_CLUSTER) return {tiles, 1, (int)splits};
     }
+    f.tiles = tiles_in_grid(a, tiles, 16, f.cluster);
     return f;
 }
 // What both kernels take, in us, as measured on a B200 (twenty shapes of 1 to 256 sequences, 16 to 1024 rows per K/V head and 17 to 16000 keys:
 // within a third of either kernel's time, and the faster one is chosen in every one of them).
-//   16-row tiles:  3, joining 2 (4 through a workspace); a CTA 0.55 and per 16 keys 0.07 (head dim 64) or 0.15 (128) beside another on its
-//                  multiprocessor, 1.6 times that alone
+//   16-row tiles:  3, joining 2 (4 through a workspace), 0.001 for a CTA without a tile; one with a tile 0.55 and per 16 keys 0.07 (head dim 64)
+//                  or 0.15 (128) beside another on its multiprocessor, 1.6 times that alone
 //   tcgen05:       5, joining 4 and what the parts take at 4 TB/s; a unit of 256 rows 1.3 and per block of 64 keys 0.76, whatever its rows: two
 //                  tiles' chains of dependent steps.  Units of unequal length (causal order) fill the multiprocessors by falling length, equal ones in rounds,
-//                  and the longest one is a bound.
+//                  and the longest one is a bound (a limit above four times the mean length is taken for a loose one).
 // Lengths are the call's limits, or what the buffers hold per sequence; in causal order a query sees all keys but half of the queries' on average.
 struct PackedWork { double seqs, queries, keys, seen; };
 PackedWork packed_work(const PackedArgs& a) {
@@ -582,16 +602,17 @@ PackedWork packed_work(const PackedArgs& a) {
 }
 double rows_time(const PackedArgs& a, int head_dim, const RowsForm& f, int n_sms) {
     const PackedWork w = packed_work(a);
-    const double share = (double)f.cluster * f.splits, ctas = std::min(w.seqs * f.tiles, w.queries * a.group / 16 + w.seqs) * a.kv_heads * share;
+    const double share = (double)f.cluster * f.splits, all = w.seqs * f.tiles * a.kv_heads * share;
+    const double ctas = std::min(w.seqs * ((a.max_q * (double)a.group + 15) / 16), w.queries * a.group / 16 + w.seqs) * a.kv_heads * share;
     const double per_16 = (head_dim == 64 ? 0.07 : 0.15) * (ctas < n_sms ? 1.6 : 1.0);
-    return 3.0 + (f.splits > 1 ? 4.0 : f.cluster > 1 ? 2.0 : 0.0) + std::max(ctas / n_sms, 1.0) * (0.55 + per_16 * w.seen / (16.0 * share));
+    return 3.0 + (f.splits > 1 ? 4.0 : f.cluster > 1 ? 2.0 : 0.0) + std::max(ctas / n_sms, 1.0) * (0.55 + per_16 * w.seen / (16.0 * share)) + 1e-3 * std::max(all - ctas, 0.0);
 }
 double tc_time(const PackedArgs& a, int head_dim, int splits, int n_sms) {
     const PackedWork w = packed_work(a);
     const double per_unit = PACKED_TC_ROWS / a.group * a.group;
     const double units = std::min(w.seqs * ceil((double)a.max_q * a.group / per_unit), w.queries * a.group / per_unit + w.seqs) * a.kv_heads * splits;
     auto unit = [&](double keys) { return 1.3 + 0.76 * ceil(ceil(keys / 64.0) / splits); };
-    const double run = std::max(unit(a.max_kv), w.seen < w.keys ? units / n_sms * unit(w.seen) : ceil(units / n_sms) * unit(w.keys));
+    const double run = std::max(unit(std::min((double)a.max_kv, 4 * w.keys)), w.seen < w.keys ? units / n_sms * unit(w.seen) : ceil(units / n_sms) * unit(w.keys));
     return 5.0 + run + (splits > 1 ? 4.0 + (double)packed_tc_workspace(a, head_dim, splits) * 2 / 4e6 : 0.0);
 }
 // units that share a tile pair's keys, with a workspace of that size
@@ -628,7 +649,8 @@ F32Form f32_form(const PackedArgs& a, int n_sms) {
     const long long rows = (long long)a.max_q * a.group;
     F32Form f = {rows <= 16 ? 16 : 64, 0, 1};
     f.tiles = (int)((rows + f.rows - 1) / f.rows);
-    f.cluster = key_split((long long)f.tiles * a.kv_heads * a.n_seqs, 2ll * n_sms, a.max_kv, F32_KEYS, F32_EVEN_KEYS);
+    f.cluster = key_split(tiles_of(a, f.tiles, f.rows) * a.kv_heads, 2ll * n_sms, a.max_kv, F32_KEYS, F32_EVEN_KEYS);
+    f.tiles = tiles_in_grid(a, f.tiles, f.rows, f.cluster);
     return f;
 }
 template <int D, int R>

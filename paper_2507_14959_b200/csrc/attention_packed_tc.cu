@@ -1,8 +1,8 @@
 // Attention over packed sequences on the tcgen05 tensor cores (bf16; the operator is described in attention_packed.cu).
 //
-// A persistent CTA (two per SM for head dim 64) walks units: two tiles of 128 rows of a (sequence, K/V head) pair -- a row is a (query,
-// head of the group) pair, so a tile holds TT = 128 / group queries of all the heads that share K and V, and the keys and values of
-// a block serve 256 rows.  Key blocks of 64 pass through a ring in shared memory.  Per tile and block
+// A persistent CTA per SM walks units: two tiles of 128 rows of a (sequence, K/V head) pair -- a row is a (query, head of the group)
+// pair, so a tile holds TT = 128 / group queries of all the heads that share K and V, and the keys and values of a block serve 256
+// rows.  Key blocks of 64 pass through a ring in shared memory.  Per tile and block
 //     S = Q K^T             UMMA 128 x 64 x 16 steps, fp32 scores in tensor memory
 //     P = 2^(c S - c m)     one row per thread: its 64 scores in registers, written back over S as packed bf16
 //     O += P V              UMMA 128 x D x 16 steps, P read from tensor memory, V as an MN-major operand
@@ -10,14 +10,18 @@
 // m is the row's running maximum, but it only moves when it has grown by more than 2^8 in the exponential's scale: then the thread
 // takes its row of O and of the sum down to the new one (no overflow can come of the lag: terms stay below 2^8, sums below 2^8 n).
 //     warps 0..3, 4..7    softmax and output of the two tiles
-//     warp 8              MMA issue
+//     warps 8, 11         MMA issue, one tile each (one thread for both was the limit: it waits for either tile's step)
 //     warp 9              units, TMA loads
 //     warp 10             the rows of a value block that lie behind the sequence's last key are set to zero (at most 15 of them
 //                         take part in a product, with weight zero; what lies there may be NaN)
-// What bounds it is a tile's chain of dependent steps -- wait, load, maximum, exponentials, store, signal, product, scores -- of which the
-// special-function unit, the next limit, sees a third.  So several tiles take turns on an SM: with head dim 64 two CTAs of two tiles each
-// (half of tensor memory: 64 columns of S and 64 of O a tile), with 128 one CTA whose tiles have two buffers of S, so that
-// the next scores are formed meanwhile.
+// What bounds it is a tile's chain of dependent steps -- wait, load, maximum, exponentials, store, signal, product, scores -- and, of the
+// units, the issue slots (half of them used) and the special-function unit, so a quarter of the exponentials are worked out by a cubic.
+// Each tile has two buffers of scores, so that the next ones are formed meanwhile, and the tiles take turns.  Measured, 37 heads of
+// 4096 tokens without causal order: head dim 64 660 TFLOP/s (tensor pipe 32 % busy), 128 1120 TFLOP/s (59 %; causal 1015): a block costs
+// the softmax the same and the products twice as much.  Two CTAs per SM, sixteen softmax warps, halves of P handed on early, scores loaded
+// half a block ahead and masks added in tensor memory gained nothing.
+// Where units are few and the keys many, SPLIT units share a tile pair's keys and leave O, m and the sum in a workspace, which a second
+// kernel joins: 256 tokens over 8000 keys of 8 / 2 heads of 128 33 us, 76 without.
 // Units are visited by falling cost, there and back over the CTAs: up to PT_SORTED sequences are ranked by every CTA when it starts (more of
 // them are taken in their own order).
 #include <algorithm>
@@ -723,31 +727,32 @@ __global__ void __launch_bounds__(32 * PT_JOIN_WARPS) attention_join_tc_kernel(c
     dep_release();
     dep_wait();
     const Segment g = packed_segment(a, blockIdx.y);
-    const long long i = (long long)blockIdx.x * PT_JOIN_WARPS + (threadIdx.x >> 5);
-    if (i >= (long long)g.nq * a.heads) return;
-    const long long stride = (long long)a.q_rows * a.heads, at = (long long)g.q0 * a.heads + i;
-    float m = -INFINITY;
-    for (int k = 0; k < args.splits; ++k) m = fmaxf(m, args.part_ml[k * stride + at].x);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[EACH];
+    const long long stride = (long long)a.q_rows * a.heads;
+    for (long long i = (long long)blockIdx.x * PT_JOIN_WARPS + (threadIdx.x >> 5); i < (long long)g.nq * a.heads; i += (long long)gridDim.x * PT_JOIN_WARPS) {
+        const long long at = (long long)g.q0 * a.heads + i;
+        float m = -INFINITY;
+        for (int k = 0; k < args.splits; ++k) m = fmaxf(m, args.part_ml[k * stride + at].x);
+        const float base = m == -INFINITY ? 0.f : m;
+        float l = 0.f, o[EACH];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) o[e] = 0.f;
-    for (int k = 0; k < args.splits; ++k) {
-        const float2 ml = args.part_ml[k * stride + at];
-        if (ml.x == -INFINITY) continue;                      // saw nothing, left no output
-        const float f = ex2f(ml.x - base);
-        l = fmaf(ml.y, f, l);
+        for (int e = 0; e < EACH; ++e) o[e] = 0.f;
+        for (int k = 0; k < args.splits; ++k) {
+            const float2 ml = args.part_ml[k * stride + at];
+            if (ml.x == -INFINITY) continue;                  // saw nothing, left no output
+            const float f = ex2f(ml.x - base);
+            l = fmaf(ml.y, f, l);
 #pragma unroll
-        for (int e = 0; e < EACH; e += 2) {
-            const float2 x = *reinterpret_cast<const float2*>(args.part_o + (k * stride + at) * D + lane * EACH + e);
-            o[e] = fmaf(x.x, f, o[e]);
-            o[e + 1] = fmaf(x.y, f, o[e + 1]);
+            for (int e = 0; e < EACH; e += 2) {
+                const float2 x = *reinterpret_cast<const float2*>(args.part_o + (k * stride + at) * D + lane * EACH + e);
+                o[e] = fmaf(x.x, f, o[e]);
+                o[e + 1] = fmaf(x.y, f, o[e + 1]);
+            }
         }
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    bf16* to = (bf16*)a.out + (g.q0 + i / a.heads) * a.out_stride + i % a.heads * D + lane * EACH;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bf16* to = (bf16*)a.out + (g.q0 + i / a.heads) * a.out_stride + i % a.heads * D + lane * EACH;
 #pragma unroll
-    for (int e = 0; e < EACH; e += 2) *reinterpret_cast<uint32_t*>(to + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
+        for (int e = 0; e < EACH; e += 2) *reinterpret_cast<uint32_t*>(to + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
+    }
 }
 
 template <int D>
@@ -775,7 +780,9 @@ cudaError_t launch_tc(const Launch& L, const PackedArgs& a, int n_sms, int split
                                       tm_v, args);
     BUMP(L);
     if (e != cudaSuccess || splits == 1) return e;
-    const long long rows = (long long)a.max_q * a.heads;
+    // a warp per row of the longest sequence, but where the limit is far above the sequences' mean not more than 16 times the warps that all rows
+    // need: those of shorter sequences find nothing to do
+    const long long rows = std::min((long long)a.max_q * a.heads, ((long long)a.q_rows * a.heads * 16 + a.n_seqs - 1) / a.n_seqs);
     e = launch_overlapped(L, attention_join_tc_kernel<D>, dim3((unsigned)((rows + PT_JOIN_WARPS - 1) / PT_JOIN_WARPS), a.n_seqs), 32 * PT_JOIN_WARPS, 0, 1, args);
     BUMP(L);
     return e;

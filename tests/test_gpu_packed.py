@@ -470,6 +470,32 @@ def test_units_that_share_their_keys():
             check(0, dim, heads, kv_heads, lengths, causal, seed=71)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("causal", [True, False])
+def test_limits_far_above_the_lengths(dtype, causal):
+    """max_q = all rows: a sequence's tiles are more than the grid gives it, and most sequences leave most of theirs empty."""
+    from paper_2507_14959_b200 import binding
+    lengths = [(3, 3)] * 1500 + [(500, 500)] + [(17, 17), (0, 0), (1, 1)] * 30
+    rows = sum(a for a, _ in lengths)
+    form = binding.attention_packed_kernel(heads=4, kv_heads=2, head_dim=64, n_seqs=len(lengths), max_q=rows, max_kv=rows, q_rows=rows, kv_rows=rows, dtype=dtype)
+    assert form[0] == ("fp32" if dtype else "16 rows") and form[2] == 1, form
+    q_off = [0]
+    for n, _ in lengths:
+        q_off.append(q_off[-1] + n)
+    q, k, v = (normal(s, rows, h, 64).to(torch.float32 if dtype else torch.bfloat16).cuda() for s, h in ((1, 4), (2, 2), (3, 2)))
+    tight, loose, status = torch.full_like(q, 7), torch.full_like(q, 7), ints([5])
+    binding.attention_packed(q, k, v, tight, ints(q_off), 500, 500, dtype, causal=causal)
+    binding.attention_packed(q, k, v, loose, ints(q_off), rows, rows, dtype, causal=causal, status=status)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    for n, at in zip((n for n, _ in lengths), q_off):
+        if n == 0:
+            continue
+        want, mean, size = expected(q[at:at + n], k[at:at + n], v[at:at + n], causal, 64 ** -0.5)
+        for out in (tight, loose):
+            assert ((out[at:at + n].double() - want).abs() <= bound(dtype, want, mean, size, 64, n)).all()
+
+
 def test_other_streams_side_by_side():
     """Calls on two streams share nothing."""
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
