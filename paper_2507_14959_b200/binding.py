@@ -482,6 +482,7 @@ def intra_coherence(contexts, co_norm):
 # struct with one pack.
 _types = None                  # element types by dtype
 _int32 = _float32 = None
+MAX_ROWS = 2 ** 31 - 1         # the library counts them in 32 bits
 _device = None                 # () -> current device ordinal
 
 
@@ -514,14 +515,17 @@ def _on(where, name, t, here, dtype):
 
 
 def _heads(where, name, t):
-    """(rows, heads, head_dim, elements between rows) of [rows, heads, head_dim] whose heads lie side by side in a row."""
+    """(rows, heads, head_dim, elements between rows) of [rows, heads, head_dim] whose heads lie side by side in a row; up to one row is
+    at any distance from the next."""
     shape = t.shape
     if len(shape) != 3:
         _refuse(where, f"{name} is not [rows, heads, head_dim]")
     (rows, heads, dim), (row, head, element) = shape, t.stride()
     if (element != 1 and dim > 1) or (head != dim and heads > 1):
         _refuse(where, f"the heads of a row of {name} do not lie side by side")
-    return rows, heads, dim, row if rows > 1 else max(row, heads * dim)
+    if rows > MAX_ROWS:
+        _refuse(where, f"{name} has {rows} rows")
+    return rows, heads, dim, row if rows > 1 or (row >= heads * dim and row % 8 == 0) else heads * dim
 
 
 def _indexes(where, name, t, here, *lengths):
@@ -582,6 +586,13 @@ _ATTENTION_ARGS = struct.Struct("@4P4q3P9ifiPPN")          # pm_packed_attention
 assert _NORM_ARGS.size == C.sizeof(pm_qk_norm_rope_args) and _ATTENTION_ARGS.size == C.sizeof(pm_packed_attention)
 
 
+def _pack(where, layout, *fields):
+    try:
+        return layout.pack(*fields)
+    except (struct.error, OverflowError) as e:             # a number that its field does not hold
+        _refuse(where, e)
+
+
 def _weights(where, name, t, here, heads, dim, per_head):
     """Address of fp32 weights [head_dim], or [heads, head_dim]; 0 for none."""
     if t is None:
@@ -618,7 +629,8 @@ def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_be
         kos, kp, kop = k_shape[3], k.data_ptr(), k_out.data_ptr()
     if q_shape[:3] != (rows, heads, dim) or (table is not None and dim != table.head_dim):
         _refuse(where, "shapes differ")
-    args = _NORM_ARGS.pack(
+    args = _pack(
+        where, _NORM_ARGS,
         q.data_ptr(), kp, q_out.data_ptr(), kop, qs, ks, q_shape[3], kos,
         _weights(where, "q_gamma", q_gamma, here, heads, dim, per_head), _weights(where, "k_gamma", k_gamma, here, kv_heads, dim, per_head),
         _weights(where, "q_beta", q_beta, here, heads, dim, per_head), _weights(where, "k_beta", k_beta, here, kv_heads, dim, per_head),
@@ -646,7 +658,9 @@ def _workspace(lib, args, like, stream):
     if stream is None:
         return torch.empty(need.value, dtype=torch.uint8, device=like.device)
     # what torch gives out on the current stream may still be in use there when another stream gets to it
-    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream))):
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream_ptr(stream)) if _stream_ptr(stream) > 1 else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
         return torch.empty(need.value, dtype=torch.uint8, device=like.device)
 
 
@@ -680,10 +694,7 @@ def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offset
         sp = _indexes(where, "status", status, here, 1)
     fields = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), qs, ks, v_shape[3], o_shape[3], qo, ko, kl, rows, kv_rows, n, max_q, max_kv, heads,
               kv_heads, dim, 1 if causal else 0, 0.0 if scale is None else scale, dtype, sp)
-    try:
-        args = _ATTENTION_ARGS.pack(*fields, 0, 0)
-    except struct.error as e:
-        _refuse(where, e)
+    args = _pack(where, _ATTENTION_ARGS, *fields, 0, 0)
     if max_kv >= LONG_HISTORY and dtype == 0 and (n * kv_heads + rows * heads // 128) <= MANY_UNITS:
         space = _workspace(lib, args, q, stream)
         if space is not None:

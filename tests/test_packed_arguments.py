@@ -163,6 +163,22 @@ def test_the_binding_reads_shapes_and_distances(lib):
             binding._heads("x", "q", bad)
 
 
+def test_the_binding_refuses_what_the_library_cannot_count(lib):
+    """Numbers beyond a field of the argument structs are refused, not cut short; one row may lie at any distance from the next."""
+    import torch
+    for field in (2 ** 31, "3", 1.5, None):
+        with pytest.raises(binding.PolymorphError) as e:
+            binding._pack("x", binding._ATTENTION_ARGS, *([64] * 19 + [field] + [0] * (len(binding.pm_packed_attention._fields_) - 20)))
+        assert e.value.code == binding.PM_ERR_ARG
+    values = [0] * len(binding.pm_packed_attention._fields_)
+    values[[n for n, _ in binding.pm_packed_attention._fields_].index("scale")] = 10 ** 400
+    with pytest.raises(binding.PolymorphError):
+        binding._pack("x", binding._ATTENTION_ARGS, *values)
+    with pytest.raises(binding.PolymorphError):
+        binding._heads("x", "q", torch.zeros((1, 1, 16)).expand(2 ** 31, 1, 16))
+    assert binding._heads("x", "q", torch.zeros(3 * 64 + 1)[1:].as_strided((1, 3, 64), (7, 64, 1))) == (1, 3, 64, 192)
+
+
 # ---- which kernel a call takes ---------------------------------------------------------------------
 @pytest.mark.parametrize("sizes,form", [
     # one frame: tiles of 16 rows; sixteen: units of 256
