@@ -250,11 +250,12 @@ __global__ void __launch_bounds__(32 * ROWS_WARPS) attention_rows_kernel(const _
                 }
             }
             if (splits > 1) {
+                if (r0 + row >= rows) return;                               // all tiles are in the grid
                 RowsPart<D>& part = parts[((size_t)(blockIdx.z * a.kv_heads + h) * in_grid + tile) * splits + rank];
 #pragma unroll
                 for (int e = 0; e < EACH; e += 4) *reinterpret_cast<float4*>(&part.o[row][c0 + e * 8]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
                 if ((threadIdx.x & 7) == 0) { part.m[row] = m; part.l[row] = l; }
-                return;                                                     // all tiles are in the grid
+                return;
             }
             if (cluster == 1) {
                 const int r = r0 + row;
