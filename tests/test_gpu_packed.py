@@ -470,6 +470,42 @@ def test_units_that_share_their_keys():
             check(0, dim, heads, kv_heads, lengths, causal, seed=71)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("queries,form", [(700, "tcgen05"), (2, "16 rows")])
+def test_parts_in_a_workspace_that_held_something_else(queries, form, causal):
+    """The library itself, with a workspace full of NaN: sequences without keys and rows that see nothing give zeros, a malformed sequence's rows stay, a
+    NaN stays in its row, nothing behind the workspace is written."""
+    import ctypes as C
+    from paper_2507_14959_b200 import binding
+    heads, kv_heads, dim, n = 4, 2, 64, 9000
+    lengths, long_last = [(queries, n), (queries, 0), (queries, queries // 2), (queries, 70)], (queries, 5000)
+    q_at = np.cumsum([0] + [a for a, _ in lengths] + [queries])
+    k_at = np.cumsum([0] + [b for _, b in lengths])
+    rows, kv_rows = int(q_at[-1]), int(k_at[-1])
+    q, k, v = normal(1, rows, heads, dim).bfloat16().cuda(), normal(2, kv_rows, kv_heads, dim).bfloat16().cuda(), normal(3, kv_rows, kv_heads, dim).bfloat16().cuda()
+    q[1, 2] = math.nan
+    # the last sequence's keys would lie behind the buffer
+    q_off, k_off, counts = ints(q_at.tolist()), ints(k_at.tolist()), ints([b for _, b in lengths] + [long_last[1]])
+    out, status = torch.full_like(q, FILL), ints([0])
+    lib, sms, need = binding.load(), torch.cuda.get_device_properties(0).multi_processor_count, C.c_size_t(0)
+    fields = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), heads * dim, kv_heads * dim, kv_heads * dim, heads * dim, q_off.data_ptr(), k_off.data_ptr(),
+              counts.data_ptr(), rows, kv_rows, len(lengths) + 1, queries, n, heads, kv_heads, dim, int(causal), 0.0, 0, status.data_ptr())
+    assert lib.pm_attention_packed_workspace(binding._ATTENTION_ARGS.pack(*fields, 0, 0), sms, C.byref(need)) == 0 and need.value > 0
+    space = torch.full((need.value + 4096,), 255, dtype=torch.uint8, device="cuda")         # every float a NaN
+    packed, took = binding._ATTENTION_ARGS.pack(*fields, space.data_ptr(), need.value), (C.c_int32 * 3)()
+    assert lib.pm_attention_packed_kernel(packed, sms, took) == 0 and (took[0], took[2] > 1) == (("16 rows", "tcgen05").index(form), True)
+    assert lib.pm_attention_packed(packed, binding._stream_ptr(None)) == 0
+    torch.cuda.synchronize()
+    assert status.item() == binding.PM_ERR_ARG and (out[rows - queries:] == FILL).all() and (space[need.value:] == 255).all()
+    assert torch.isnan(out[1, 2]).all()
+    out[1, 2] = q[1, 2] = 0
+    for (a, b), x, y in zip(lengths, q_at, k_at):
+        want, mean, size = expected(q[x:x + a], k[y:y + b], v[y:y + b], causal, dim ** -0.5)
+        if x == 0:
+            want[1, 2] = 0
+        assert ((out[x:x + a].double() - want).abs() <= bound(0, want, mean, size, dim, max(b, 1))).all(), (a, b)
+
+
 @pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("causal", [True, False])
 def test_limits_far_above_the_lengths(dtype, causal):

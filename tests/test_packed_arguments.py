@@ -192,6 +192,10 @@ def test_the_binding_refuses_what_the_library_cannot_count(lib):
     (dict(heads=32, kv_heads=8, head_dim=128, n_seqs=48, max_q=1, max_kv=8192), ("16 rows", 4, 1)),
     (dict(heads=32, kv_heads=8, head_dim=128, n_seqs=48, max_q=1, max_kv=300), ("16 rows", 1, 1)),
     (dict(heads=32, kv_heads=8, head_dim=128, n_seqs=3, max_q=8192, max_kv=8192), ("tcgen05", 1, 1)),
+    # units of too few rows share their keys where there is a workspace
+    (dict(heads=8, kv_heads=2, head_dim=128, n_seqs=1, max_q=256, max_kv=8000, workspace_bytes=1 << 28), ("tcgen05", 1, 7)),
+    # a limit far above the lengths does not change the kernel
+    (dict(heads=12, kv_heads=12, head_dim=64, n_seqs=512, max_q=100864, max_kv=100864, q_rows=100864, kv_rows=100864), ("tcgen05", 1, 1)),
     (dict(heads=6, kv_heads=6, head_dim=64, n_seqs=8, max_q=577, max_kv=577, dtype=1), ("fp32", 2, 1)),
     (dict(heads=6, kv_heads=6, head_dim=64, n_seqs=8, max_q=0, max_kv=577), ("none", 1, 1))])
 def test_kernel_of_a_call(lib, sizes, form):
