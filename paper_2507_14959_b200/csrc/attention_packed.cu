@@ -358,15 +358,19 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) attention_join_kernel(const _
 // ---------------------------------------------------------------------------------------
 // fp32 on CUDA cores: R rows (64, or 16 where there are few) per CTA, keys 64 at a time.  256 threads as 16 x 16: thread (ty, tx) forms
 // the scores of rows ty + 16 i and keys tx + 16 j and the output of its rows at columns 4 tx + 64 j.  Rows of Q and K lie D + 4 floats
-// apart, so that the 16-byte reads of eight neighbouring threads touch all banks once; P takes the place of K.  Products run packed, two
+// apart, so that the 16-byte reads of eight neighbouring threads touch all banks once; with 64 rows P takes the place of K.  Products run packed, two
 // results per instruction: one at a time the floating-point unit gives half its rate.
 // ---------------------------------------------------------------------------------------
 constexpr int F32_KEYS = 64;
 template <int D, int R>
 struct F32Smem {
+    // Few rows: P has a place of its own, and the next keys are fetched meanwhile (8 streams of 8 / 2 heads of 64, a token each over 8000
+    // keys: 40.1 -> 34.2 us).  With 64 rows two CTAs cover one another's copies, and it costs 2 %.
+    static constexpr bool AHEAD = R == 16;
     float q[R][D + 4];
-    float k[F32_KEYS][D + 4];            // then P: [R][F32_KEYS + 4]
+    float k[F32_KEYS][D + 4];            // unless AHEAD, then P: [R][F32_KEYS + 4]
     float v[F32_KEYS][D];
+    float p[AHEAD ? R : 1][F32_KEYS + 4];
     float m[R], l[R];
 };
 
@@ -375,8 +379,9 @@ __global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_cons
     constexpr int RT = R / 16, DT = D / 64;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     F32Smem<D, R>& sm = *reinterpret_cast<F32Smem<D, R>*>(smem_raw);
+    constexpr bool AHEAD = F32Smem<D, R>::AHEAD;
     static_assert(R * (F32_KEYS + 4) <= F32_KEYS * (D + 4), "P fits the keys");
-    float (*ps)[F32_KEYS + 4] = reinterpret_cast<float (*)[F32_KEYS + 4]>(&sm.k[0][0]);
+    float (*ps)[F32_KEYS + 4] = AHEAD ? sm.p : reinterpret_cast<float (*)[F32_KEYS + 4]>(&sm.k[0][0]);
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int rank = blockIdx.x % cluster, in_grid = gridDim.x / cluster, h = blockIdx.y;
     dep_release();
@@ -407,17 +412,30 @@ __global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_cons
         const bool active = R > 16 || r0 + (ty & ~1) < rows;
         const float* kp = (const float*)a.k + (long long)seg.k0 * a.k_stride + h * D;
         const float* vp = (const float*)a.v + (long long)seg.k0 * a.v_stride + h * D;
-        for (int b0 = rank * F32_KEYS; b0 < k_end; b0 += cluster * F32_KEYS) {
-            __syncthreads();                                                // the block before has been read
-            for (int i = threadIdx.x; i < F32_KEYS * D / 4; i += 256) {
-                const int r = i / (D / 4), c = i % (D / 4) * 4, key = b0 + r;
-                const bool real = key < k_end;
-                const long long row = real ? key : 0;
-                copy16(smem_u32(&sm.k[r][c]), kp + row * a.k_stride + c, real);
-                copy16(smem_u32(&sm.v[r][c]), vp + row * a.v_stride + c, real);
-            }
+        auto fetch = [&](bool keys, bool values, int b0) {
+            if (b0 < k_end)
+                for (int i = threadIdx.x; i < F32_KEYS * D / 4; i += 256) {
+                    const int r = i / (D / 4), c = i % (D / 4) * 4, key = b0 + r;
+                    const bool real = key < k_end;
+                    const long long row = real ? key : 0;
+                    if (keys) copy16(smem_u32(&sm.k[r][c]), kp + row * a.k_stride + c, real);
+                    if (values) copy16(smem_u32(&sm.v[r][c]), vp + row * a.v_stride + c, real);
+                }
             copy_commit();
-            copy_wait<0>();
+        };
+        const int hop = cluster * F32_KEYS;
+        if (AHEAD) {
+            fetch(true, false, rank * F32_KEYS);
+            fetch(false, true, rank * F32_KEYS);
+        }
+        for (int b0 = rank * F32_KEYS; b0 < k_end; b0 += hop) {
+            if (AHEAD) {
+                copy_wait<1>();                                             // the keys
+            } else {
+                __syncthreads();                                            // the block before has been read
+                fetch(true, true, b0);
+                copy_wait<0>();
+            }
             __syncthreads();
             float s[RT][4];
             if (active) {
@@ -445,7 +463,8 @@ __global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_cons
                         s[i][j] = a0 + a1;
                     }
             }
-            __syncthreads();                                                // P goes where the keys were
+            __syncthreads();                                                // the keys have been read; P goes where they were
+            if (AHEAD) fetch(true, false, b0 + hop);
             if (active) {
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {
@@ -470,6 +489,7 @@ __global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_cons
                     for (int j = 0; j < DT; ++j) { o[i][j][0] = mul2(o[i][j][0], pk2(f, f)); o[i][j][1] = mul2(o[i][j][1], pk2(f, f)); }
                 }
             }
+            if (AHEAD) copy_wait<1>();                                      // the values
             __syncthreads();
             if (active) {
 #pragma unroll 2
@@ -496,6 +516,10 @@ __global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_cons
                         }
                     }
                 }
+            }
+            if (AHEAD) {
+                __syncthreads();                                            // the block has been read
+                fetch(false, true, b0 + hop);
             }
         }
 #pragma unroll
