@@ -481,7 +481,7 @@ typedef struct {
 #define PM_PACKED_MAX_SEQS 4096
 #define PM_PACKED_MAX_GROUP 64
 /* Errors: PM_ERR_ARG (NULL, ranges, alignment), PM_ERR_CAPACITY (n_seqs, heads / kv_heads, kv_heads > 65535, max_q * heads / kv_heads >= 2^30),
- * PM_ERR_CUDA.  Nothing is launched on error. */
+ * PM_ERR_CUDA.  Nothing is launched on the first two; with PM_ERR_CUDA a part of the call may have been, and out is then not complete. */
 int pm_attention_packed(const pm_packed_attention* args, void* cuda_stream);
 
 /* Host function (needs no GPU; n_sms: multiprocessors of the one that will run the call): bytes of workspace with which calls of few rows, or of

@@ -15,7 +15,7 @@ namespace {
 
 #define CK(expr)                                                                        \
     do {                                                                                \
-        cudaError_t _e = (expr);                                                        \
+        cudaError_t _e = consumed(expr);                                                \
         if (_e != cudaSuccess) {                                                        \
             err = std::string(#expr) + ": " + cudaGetErrorString(_e);                   \
             return _e == cudaErrorMemoryAllocation ? PM_ERR_OOM : PM_ERR_CUDA;          \
@@ -34,7 +34,7 @@ struct DevBuf {              // owning device allocation
         if (p) { cudaFree(p); p = nullptr; }
         bytes = n;
         if (n == 0) return cudaSuccess;
-        return cudaMalloc(&p, n);
+        return consumed(cudaMalloc(&p, n));
     }
     template <typename T> T* as() const { return reinterpret_cast<T*>(p); }
 };
@@ -45,7 +45,7 @@ cudaError_t upload(DevBuf& buf, const float* host, size_t n) {
     if (e != cudaSuccess) return e;
     std::vector<T> tmp(n);
     for (size_t i = 0; i < n; ++i) tmp[i] = host_cvt<T>(host[i]);
-    return cudaMemcpy(buf.p, tmp.data(), n * sizeof(T), cudaMemcpyHostToDevice);
+    return consumed(cudaMemcpy(buf.p, tmp.data(), n * sizeof(T), cudaMemcpyHostToDevice));
 }
 
 // [k_in, n_out] row-major -> [n_out, k_in]
@@ -56,7 +56,7 @@ cudaError_t upload_transposed(DevBuf& buf, const float* w, int k_in, int n_out) 
     std::vector<T> tmp((size_t)k_in * n_out);
     for (int k = 0; k < k_in; ++k)
         for (int n = 0; n < n_out; ++n) tmp[(size_t)n * k_in + k] = host_cvt<T>(w[(size_t)k * n_out + n]);
-    return cudaMemcpy(buf.p, tmp.data(), tmp.size() * sizeof(T), cudaMemcpyHostToDevice);
+    return consumed(cudaMemcpy(buf.p, tmp.data(), tmp.size() * sizeof(T), cudaMemcpyHostToDevice));
 }
 
 size_t esize(int dtype) { return dtype == 0 ? 2 : 4; }
@@ -405,7 +405,7 @@ int fetch_csr(const int32_t* offsets, const int32_t* ids, int n_frames, cudaStre
     *o = offsets; *i = ids;
     if (!offsets || n_frames <= 0) return PM_OK;
     cudaPointerAttributes at;
-    if (cudaPointerGetAttributes(&at, offsets) != cudaSuccess) { cudaGetLastError(); return PM_OK; }
+    if (consumed(cudaPointerGetAttributes(&at, offsets)) != cudaSuccess) return PM_OK;
     if (at.type != cudaMemoryTypeDevice) return PM_OK;
     hoff.resize(n_frames + 1);
     CK(cudaMemcpyAsync(hoff.data(), offsets, sizeof(int32_t) * (n_frames + 1), cudaMemcpyDeviceToHost, st));
@@ -877,7 +877,7 @@ int pm_create(const pm_config* cfg, const pm_backbone* w, pm_handle* out) {
     h->slabs_max = slabs_for(c.max_rank);
     int dev = 0;
     cudaGetDevice(&dev);
-    if (cudaDeviceGetAttribute(&h->n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    if (consumed(cudaDeviceGetAttribute(&h->n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) {
         delete h; return PM_ERR_CUDA;
     }
     h->ranks.assign(std::max(1, c.max_adapters), 0);
@@ -891,11 +891,11 @@ int pm_create(const pm_config* cfg, const pm_backbone* w, pm_handle* out) {
     if (h->scale_dev.alloc(h->scales.size() * sizeof(float)) != cudaSuccess ||
         h->rank_dev.alloc(h->ranks.size() * sizeof(int)) != cudaSuccess ||
         h->status.alloc(sizeof(int)) != cudaSuccess ||
-        cudaMemset(h->status.p, 0, sizeof(int)) != cudaSuccess) { err = "allocation failed"; return fail(PM_ERR_OOM); }
+        consumed(cudaMemset(h->status.p, 0, sizeof(int))) != cudaSuccess) { err = "allocation failed"; return fail(PM_ERR_OOM); }
     rc = sync_meta(h->scale_dev, h->rank_dev, h->scales, h->ranks, err);
     if (rc) return fail(rc);
     h->meta.scale = h->scale_dev.as<float>(); h->meta.rank = h->rank_dev.as<int>();
-    if (cudaDeviceSynchronize() != cudaSuccess) { err = "device synchronize failed"; return fail(PM_ERR_CUDA); }
+    if (consumed(cudaDeviceSynchronize()) != cudaSuccess) { err = "device synchronize failed"; return fail(PM_ERR_CUDA); }
     *out = h;
     return PM_OK;
 }
@@ -1249,14 +1249,14 @@ int pm_linear_create(int k_in, int n_out, const float* w, const float* bias, int
     cudaError_t e = l->scale_dev.alloc(l->scales.size() * sizeof(float));
     if (e == cudaSuccess) e = l->rank_dev.alloc(l->ranks.size() * sizeof(int));
     if (e == cudaSuccess) e = l->status.alloc(sizeof(int));
-    if (e == cudaSuccess) e = cudaMemset(l->status.p, 0, sizeof(int));
+    if (e == cudaSuccess) e = consumed(cudaMemset(l->status.p, 0, sizeof(int)));
     if (e == cudaSuccess && dtype == 1)
         e = l->t32.alloc(rows * std::max(1, max_set) * std::max(1, l->slabs_max) * PM_SLAB * sizeof(float));
     size_t tb = 0;
     if (e == cudaSuccess && dtype == 0) {
         tb = (size_t)l->router.max_tiles * std::max(1, l->router.slab_cap) * PM_TILE_M * PM_SLAB;
         e = l->tbuf.alloc(tb * sizeof(bf16));
-        if (e == cudaSuccess) e = cudaMemset(l->tbuf.p, 0, l->tbuf.bytes);
+        if (e == cudaSuccess) e = consumed(cudaMemset(l->tbuf.p, 0, l->tbuf.bytes));
     }
     if (e != cudaSuccess) { err = cudaGetErrorString(e); return fail(e == cudaErrorMemoryAllocation ? PM_ERR_OOM : PM_ERR_CUDA); }
     if (dtype == 0 && !tm_encode_2d(&l->tm_t, l->tbuf.p, PM_SLAB, tb / PM_SLAB, PM_SLAB * 2, PM_SLAB, PM_TILE_M, 32)) {
@@ -1265,7 +1265,7 @@ int pm_linear_create(int k_in, int n_out, const float* w, const float* bias, int
     rc = sync_meta(l->scale_dev, l->rank_dev, l->scales, l->ranks, err);
     if (rc) return fail(rc);
     l->meta.scale = l->scale_dev.as<float>(); l->meta.rank = l->rank_dev.as<int>();
-    if (cudaDeviceSynchronize() != cudaSuccess) { err = "device synchronize failed"; return fail(PM_ERR_CUDA); }
+    if (consumed(cudaDeviceSynchronize()) != cudaSuccess) { err = "device synchronize failed"; return fail(PM_ERR_CUDA); }
     *out = l;
     return PM_OK;
 }
@@ -1371,12 +1371,12 @@ int pm_attention(const void* qkv, void* out, int n_frames, int tokens, int heads
         // (one word per device, allocated on first use)
         static std::atomic<int*> status_words[64];
         int dev = 0, n_sms = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 ||
-            cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return PM_ERR_CUDA;
+        if (consumed(cudaGetDevice(&dev)) != cudaSuccess || dev < 0 || dev >= 64 ||
+            consumed(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return PM_ERR_CUDA;
         int* status_word = status_words[dev].load(std::memory_order_acquire);
         if (!status_word) {
-            if (cudaMalloc(&status_word, sizeof(int)) != cudaSuccess) return PM_ERR_OOM;
-            if (cudaMemset(status_word, 0, sizeof(int)) != cudaSuccess) return PM_ERR_CUDA;
+            if (consumed(cudaMalloc(&status_word, sizeof(int))) != cudaSuccess) return PM_ERR_OOM;
+            if (consumed(cudaMemset(status_word, 0, sizeof(int))) != cudaSuccess) return PM_ERR_CUDA;
             int* expected = nullptr;
             if (!status_words[dev].compare_exchange_strong(expected, status_word, std::memory_order_acq_rel)) {
                 cudaFree(status_word);                    // another thread got there first

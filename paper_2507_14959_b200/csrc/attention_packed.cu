@@ -776,9 +776,9 @@ int pm_attention_packed(const pm_packed_attention* p, void* cuda_stream) {
     cudaStream_t st = (cudaStream_t)cuda_stream;
     int dev = 0, n_sms = 0;
     if (const int rc = stream_device(st, &dev); rc != PM_OK) return rc;
-    if (p->status_out && cudaMemsetAsync(p->status_out, 0, sizeof(int32_t), st) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (p->status_out && consumed(cudaMemsetAsync(p->status_out, 0, sizeof(int32_t), st)) != cudaSuccess) return PM_ERR_CUDA;
     if (a.n_seqs == 0) return PM_OK;
-    if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (consumed(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return PM_ERR_CUDA;
     a.status = p->status_out;
     Launch L;
     L.st = st;

@@ -220,16 +220,23 @@ cudaError_t launch_select(const Launch& L, const float* scores, int n_frames, in
                           int* next_off, int* next_ids, int ids_capacity,
                           unsigned long long* metrics = nullptr);   // [frames, sum |S_t|, switches] or null
 
+// A runtime call's result.  A failure stays in the thread as its last error until it is read, and a kernel launch with <<<>>> is judged by that:
+// left there, it would be taken for a later launch's own.  So whoever fails takes it away.
+inline cudaError_t consumed(cudaError_t e) {
+    if (e != cudaSuccess) cudaGetLastError();
+    return e;
+}
+
 // The current device, for an operator without a handle: a stream of another device is refused.
 inline int stream_device(cudaStream_t st, int* dev) {
-    if (cudaGetDevice(dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (consumed(cudaGetDevice(dev)) != cudaSuccess) return PM_ERR_CUDA;
     if (st == nullptr || st == cudaStreamLegacy || st == cudaStreamPerThread) return PM_OK;
     // a capture would be invalidated by the question; there, a launch into another device's stream fails by itself
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(st, &capture) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (consumed(cudaStreamIsCapturing(st, &capture)) != cudaSuccess) return PM_ERR_CUDA;
     if (capture != cudaStreamCaptureStatusNone) return PM_OK;
     int of = -1;
-    if (cudaStreamGetDevice(st, &of) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (consumed(cudaStreamGetDevice(st, &of)) != cudaSuccess) return PM_ERR_CUDA;
     return of == *dev ? PM_OK : PM_ERR_ARG;
 }
 
@@ -240,11 +247,11 @@ struct SmemGrant {
     template <typename Kernel>
     cudaError_t ensure(Kernel kernel, int bytes) {
         int dev = 0;
-        cudaError_t e = cudaGetDevice(&dev);
+        cudaError_t e = consumed(cudaGetDevice(&dev));
         if (e != cudaSuccess) return e;
         std::atomic<int>& g = granted[dev & 63];
         if (bytes <= g.load(std::memory_order_acquire)) return cudaSuccess;
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        e = consumed(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
         if (e != cudaSuccess) return e;
         int cur = g.load(std::memory_order_relaxed);
         while (cur < bytes && !g.compare_exchange_weak(cur, bytes, std::memory_order_release)) {}
@@ -331,8 +338,8 @@ cudaError_t launch_overlapped(const Launch& L, void (*kernel)(P...), dim3 grid, 
     attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    // judged by its own result: an older error of the thread says nothing about this launch
+    return consumed(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
 // tensor-map helpers (gemm_tcgen05.cu); return false if the driver entry point is unavailable

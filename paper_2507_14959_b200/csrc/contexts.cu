@@ -173,11 +173,11 @@ int pm_cooccurrence(const uint32_t* labels, int n_frames, int n_labels, float* c
     if (n_frames < 0 || n_labels <= 0 || !co || (n_frames > 0 && !labels)) return PM_ERR_ARG;
     if (n_frames > (1 << 24)) return PM_ERR_CAPACITY;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (cudaMemsetAsync(co, 0, sizeof(float) * (size_t)n_labels * n_labels, st) != cudaSuccess) return PM_ERR_CUDA;
-    if (status_out && cudaMemsetAsync(status_out, 0, sizeof(int32_t), st) != cudaSuccess) return PM_ERR_CUDA;
+    if (consumed(cudaMemsetAsync(co, 0, sizeof(float) * (size_t)n_labels * n_labels, st)) != cudaSuccess) return PM_ERR_CUDA;
+    if (status_out && consumed(cudaMemsetAsync(status_out, 0, sizeof(int32_t), st)) != cudaSuccess) return PM_ERR_CUDA;
     if (n_frames == 0) return PM_OK;
     int dev = 0, n_sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    if (consumed(cudaGetDevice(&dev)) != cudaSuccess || consumed(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
         return PM_ERR_CUDA;
     const long long entries = (long long)n_labels * (n_labels + 1) / 2;
     if (n_labels <= COOC_HIST_LABELS && n_frames >= entries) {

@@ -769,7 +769,7 @@ EncodeTiledFn get_encode() {
         tried = true;
         void* p = nullptr;
         cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+        if (consumed(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q)) == cudaSuccess &&
             q == cudaDriverEntryPointSuccess)
             fn = reinterpret_cast<EncodeTiledFn>(p);
     }
@@ -789,7 +789,7 @@ extern "C" int pm_selftest_wait_timeout(long long limit_cycles, int32_t* status,
     // the other warps' own limit is the library's (~2 s): the test limit must stay far below it
     if (!status || !trace || limit_cycles <= 0 || limit_cycles > 100000000ll) return PM_ERR_ARG;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (cudaMemsetAsync(trace, 0, 3 * sizeof(int32_t), st) != cudaSuccess) return PM_ERR_CUDA;
+    if (consumed(cudaMemsetAsync(trace, 0, 3 * sizeof(int32_t), st)) != cudaSuccess) return PM_ERR_CUDA;
     wait_timeout_selftest_kernel<<<1, 128, 0, st>>>(limit_cycles, status, trace);
     return cudaGetLastError() == cudaSuccess ? PM_OK : PM_ERR_CUDA;
 }

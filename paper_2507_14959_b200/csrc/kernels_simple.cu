@@ -802,7 +802,7 @@ cudaError_t launch_heads(const Launch& L, const T* x, int n_slots, int n_out_fra
     // one row of scores and one block per slot: it zeroes the row; else the rows are zeroed beforehand
     const bool zero_rows = sizeof(T) == 2 && n_slots == n_out_frames && parts == 1;
     if (!zero_rows) {
-        cudaError_t e = cudaMemsetAsync(scores_out, 0, (size_t)n_out_frames * n_classes * sizeof(float), L.st);
+        cudaError_t e = consumed(cudaMemsetAsync(scores_out, 0, (size_t)n_out_frames * n_classes * sizeof(float), L.st));
         if (e != cudaSuccess) return e;
     }
     if constexpr (sizeof(T) == 2) {
@@ -1105,12 +1105,12 @@ extern "C" int pm_select_static(const float* scores, int n_frames, int n_classes
     if (n_frames > PM_SELECT_STATIC_MAX_FRAMES || n_adapters > PM_SELECT_STATIC_MAX_ADAPTERS)
         return PM_ERR_CAPACITY;
     int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= STATIC_MAX_DEVICES) return PM_ERR_CUDA;
+    if (consumed(cudaGetDevice(&dev)) != cudaSuccess || dev < 0 || dev >= STATIC_MAX_DEVICES) return PM_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (st != nullptr && st != cudaStreamLegacy && st != cudaStreamPerThread) {
         // the scratch array is per device: the stream must belong to the current one
         int sdev = -1;
-        if (cudaStreamGetDevice(st, &sdev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+        if (consumed(cudaStreamGetDevice(st, &sdev)) != cudaSuccess) return PM_ERR_CUDA;
         if (sdev != dev) return PM_ERR_ARG;
     }
     if (!g_static_ready[dev].load(std::memory_order_acquire)) {
@@ -1129,8 +1129,8 @@ extern "C" int pm_select_static(const float* scores, int n_frames, int n_classes
     int* status = status_out ? status_out : g_static_scratch[dev].status;
     // what must start at zero: the status word and the kernel's block counter (word 0 of the array);
     // the mask words themselves are all rewritten before they are read
-    if (cudaMemsetAsync(status, 0, sizeof(int), st) != cudaSuccess ||
-        cudaMemsetAsync(g_static_scratch[dev].masks, 0, sizeof(uint64_t), st) != cudaSuccess)
+    if (consumed(cudaMemsetAsync(status, 0, sizeof(int), st)) != cudaSuccess ||
+        consumed(cudaMemsetAsync(g_static_scratch[dev].masks, 0, sizeof(uint64_t), st)) != cudaSuccess)
         return PM_ERR_CUDA;
     Launch L;
     L.st = st;

@@ -1313,7 +1313,7 @@ int lat_share(const LatArgs& a, size_t smem) {
     // clusters of c CTAs the device holds at once; the shared memory is that of one CTA per SM whatever the geometry
     static std::atomic<int> resident[64][LT_MAX_SHARE + 1];
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    if (consumed(cudaGetDevice(&dev)) != cudaSuccess) return 1;
     std::atomic<int>& known = resident[dev & 63][c];
     if (const int n = known.load(std::memory_order_relaxed); n > 0) return a.n_frames * a.tiles_pf <= n ? c : 1;
     cudaLaunchConfig_t cfg = {};
@@ -1327,10 +1327,7 @@ int lat_share(const LatArgs& a, size_t smem) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int clusters = 0;
-    if (cudaOccupancyMaxActiveClusters(&clusters, latency_forward_kernel<true>, &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        return 1;
-    }
+    if (consumed(cudaOccupancyMaxActiveClusters(&clusters, latency_forward_kernel<true>, &cfg)) != cudaSuccess) return 1;
     known.store(clusters, std::memory_order_relaxed);
     return a.n_frames * a.tiles_pf <= clusters ? c : 1;
 }
@@ -1372,13 +1369,13 @@ static cudaError_t launch_form(const Launch& L, const LatArgs& a, bool shared, b
     copy.status = L.status;
     copy.ring_slots = slots;
     // the frames' arrival counters start at zero (an aborted launch may have left them anywhere)
-    cudaError_t e = cudaMemsetAsync(a.bar, 0, sizeof(unsigned int) * a.n_frames * share, L.st);
+    cudaError_t e = consumed(cudaMemsetAsync(a.bar, 0, sizeof(unsigned int) * a.n_frames * share, L.st));
     if (e != cudaSuccess) return e;
-    e = share > 1 ? cudaLaunchKernelEx(&cfg, latency_forward_kernel<true>, copy) : cudaLaunchKernelEx(&cfg, latency_forward_kernel<false>, copy);
+    e = consumed(share > 1 ? cudaLaunchKernelEx(&cfg, latency_forward_kernel<true>, copy) : cudaLaunchKernelEx(&cfg, latency_forward_kernel<false>, copy));
     if (e != cudaSuccess) return e;
     launched = true;
     BUMP(L);
-    return cudaGetLastError();
+    return cudaSuccess;
 }
 
 cudaError_t launch_latency_forward(const Launch& L, const LatArgs& a) {
@@ -1389,6 +1386,5 @@ cudaError_t launch_latency_forward(const Launch& L, const LatArgs& a) {
     bool launched = false;
     const cudaError_t e = launch_form(L, a, true, launched);
     if (launched) return e;
-    if (e != cudaErrorNotSupported) cudaGetLastError();
     return launch_form(L, a, false, launched);
 }

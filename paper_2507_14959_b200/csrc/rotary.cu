@@ -302,7 +302,7 @@ int rotate(RotArgs& a, int norm, int dtype, void* cuda_stream) {
     cudaStream_t st = (cudaStream_t)cuda_stream;
     int dev = 0, n_sms = 0;
     if (const int rc = stream_device(st, &dev); rc != PM_OK) return rc;
-    if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return PM_ERR_CUDA; }
+    if (consumed(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return PM_ERR_CUDA;
     a.inv_dim = 1.f / (float)(a.units * 16);
     Launch L;
     L.st = st;

@@ -1,0 +1,52 @@
+"""Edges of the packed-sequence operators: what goes before a call, what it reports, forms that the larger tests do not reach."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_packed import bound, expected, ints, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def fail_a_call():
+    """A library call that fails on the host: adapter tables of 512 GB, refused by the allocator."""
+    from paper_2507_14959_b200 import binding
+    with pytest.raises(binding.PolymorphError) as e:
+        binding.Linear(np.zeros((64, 64), np.float32), np.zeros(64, np.float32), max_adapters=256, max_rank=1 << 24, max_set=1, max_frames=1, tokens=1)
+    assert e.value.code == binding.PM_ERR_OOM
+
+
+@pytest.mark.parametrize("queries,keys,form", [(1, 9000, ("16 rows", True)), (256, 8000, ("tcgen05", True)), (40, 40, ("16 rows", False)), (1000, 1000, ("tcgen05", False))])
+def test_attention_after_a_call_that_failed(queries, keys, form):
+    """The error of an earlier call is not taken for this one's: all of its kernels run, the one that joins the parts too."""
+    from paper_2507_14959_b200 import binding
+    heads, kv_heads, dim = 8, 2, 128
+    q, k, v = normal(1, queries, heads, dim).bfloat16().cuda(), normal(2, keys, kv_heads, dim).bfloat16().cuda(), normal(3, keys, kv_heads, dim).bfloat16().cuda()
+    out, q_off, k_off = torch.full_like(q, 7.0), ints([0, queries]), ints([0, keys])
+    took = binding.attention_packed_kernel(heads=heads, kv_heads=kv_heads, head_dim=dim, n_seqs=1, max_q=queries, max_kv=keys, workspace_bytes=1 << 28)
+    assert (took[0], took[2] > 1) == form
+    for before in (lambda: None, fail_a_call):                # the first call sets up what later ones find
+        before()
+        out.fill_(7.0)
+        binding.attention_packed(q, k, v, out, q_off, queries, keys, 0, kv_offsets=k_off, causal=True)
+    torch.cuda.synchronize()
+    want, mean, size = expected(q, k, v, True, dim ** -0.5)
+    assert ((out.double() - want).abs() <= bound(0, want, mean, size, dim, keys)).all()
+
+
+def test_other_operators_after_a_call_that_failed():
+    from paper_2507_14959_b200 import binding
+    x, table, positions, gamma = normal(1, 50, 4, 64).bfloat16().cuda(), binding.RopeTable(64), ints(list(range(50))), torch.ones(64, device="cuda")
+    f, off = x.float(), ints([0, 50])
+    weights, rows, qkv = torch.ones(256, device="cuda"), x.flatten(1).contiguous(), normal(2, 50, 3 * 64).bfloat16().cuda()
+    for like, call in ((x, lambda y: binding.rope(x, y, positions, table, 0)),
+                       (x, lambda y: binding.qk_norm_rope(x, None, y, None, gamma, None, norm="rms", eps=1e-6, dtype=0)),
+                       (f, lambda y: binding.attention_packed(f, f, f, y, off, 50, 50, 1)),
+                       (rows, lambda y: binding.layernorm(rows, weights, weights, y, 1e-6, 0)),
+                       (qkv[:, :64].contiguous(), lambda y: binding.attention(qkv, y, 1, 50, 1, 0))):
+        before, after = torch.zeros_like(like), torch.zeros_like(like)
+        call(before)
+        fail_a_call()
+        call(after)
+        torch.cuda.synchronize()
+        assert torch.equal(before, after) and before.abs().sum() > 0
