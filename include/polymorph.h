@@ -368,6 +368,11 @@ int pm_layernorm(const void* x, const float* gamma, const float* beta, void* y,
 int pm_attention(const void* qkv, void* out, int n_frames, int tokens, int heads, int dtype,
                  void* cuda_stream);
 
+/* What operators without a handle -- pm_attention, and pm_attention_packed without status_out -- have left on the current device since the
+ * last read, taken away by this call: PM_OK, PM_ERR_TIMEOUT if a bounded wait expired (rows of such a call's output are undefined), PM_ERR_ARG if
+ * sequences were skipped.  Synchronises cuda_stream, like pm_status; not for use during a capture.  Calls on other streams may still add to it. */
+int pm_operators_status(void* cuda_stream);
+
 /* ---- encoders that pack sequences of different lengths ----------------------------------- */
 /* (The paper has no counterpart: its frames are all of one size and its positions a learned table.  These operators serve
  * encoders over the same streams whose cameras differ in size, whose blocks rotate queries and keys by position, or whose new
@@ -471,9 +476,10 @@ typedef struct {
     int causal;
     float scale;                          /* > 0, or 0 for 1 / sqrt(head_dim)                                  */
     int dtype;                            /* 0 = bf16 tensor-core kernels, 1 = fp32                            */
-    int32_t* status_out;                  /* dev int32 or NULL: cleared by the call; PM_ERR_ARG if a sequence's offsets or length are
-                                             malformed, lie outside the buffers or exceed max_q / max_kv (the sequence is skipped, its
-                                             rows of out left as they were), PM_ERR_TIMEOUT if a bounded wait expired */
+    int32_t* status_out;                  /* dev int32, cleared by the call, or NULL: pm_operators_status tells.  PM_ERR_ARG if a sequence's offsets
+                                             or length are malformed, lie outside the buffers or exceed max_q / max_kv (the sequence is skipped,
+                                             its rows of out left as they were), PM_ERR_TIMEOUT if a bounded wait expired (rows of out are then
+                                             undefined) */
     void* workspace;                      /* dev, 32-byte aligned, or NULL; see pm_attention_packed_workspace  */
     size_t workspace_bytes;
 } pm_packed_attention;

@@ -25,7 +25,7 @@ EXPORTS = [
     "pm_select_static", "pm_metrics_reset", "pm_metrics_read", "pm_status", "pm_last_error", "pm_launch_count", "pm_set_graphs", "pm_set_small_batch_kernel", "pm_profile_enable", "pm_profile_read", "pm_plan_stats", "pm_linear_create", "pm_linear_register",
     "pm_linear_forward", "pm_linear_status", "pm_linear_last_error", "pm_linear_destroy",
     "pm_layernorm", "pm_attention", "pm_selftest_wait_timeout", "pm_linear_kernel", "pm_cooccurrence", "pm_build_contexts", "pm_intra_coherence",
-    "pm_rope_init", "pm_rope", "pm_qk_norm_rope", "pm_attention_packed", "pm_attention_packed_workspace", "pm_attention_packed_kernel",
+    "pm_rope_init", "pm_rope", "pm_qk_norm_rope", "pm_attention_packed", "pm_attention_packed_workspace", "pm_attention_packed_kernel", "pm_operators_status",
 ]
 
 
@@ -145,6 +145,7 @@ def load():
     lib.pm_qk_norm_rope.argtypes = [vp, vp]
     lib.pm_attention_packed.argtypes = [vp, vp]
     lib.pm_attention_packed_workspace.argtypes = [vp, ip, C.POINTER(C.c_size_t)]
+    lib.pm_operators_status.argtypes = [vp]
     lib.pm_attention_packed_kernel.argtypes = [vp, ip, C.POINTER(C.c_int32)]
     _lib = lib
     return lib
@@ -385,6 +386,12 @@ def attention(qkv, out, n_frames, tokens, heads, dtype, stream=None):
     rc = load().pm_attention(_ptr(qkv), _ptr(out), n_frames, tokens, heads, dtype, _stream_ptr(stream))
     if rc != PM_OK:
         raise PolymorphError(rc, "pm_attention")
+
+
+def operators_status(stream=None):
+    """pm_operators_status: what attention(), and attention_packed() without a status tensor, have left on the current device since the last
+    read: PM_OK, PM_ERR_TIMEOUT (a bounded wait expired) or PM_ERR_ARG (sequences with malformed lists were skipped); synchronises."""
+    return load().pm_operators_status(_stream_ptr(stream))
 
 
 def selftest_wait_timeout(limit_cycles, status, trace, stream=None):
@@ -667,7 +674,12 @@ def _workspace(lib, args, like, stream):
 def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offsets=None, kv_lengths=None, causal=False, scale=None, status=None,
                      stream=None):
     """pm_attention_packed: q, out = torch CUDA [rows, heads, head_dim], k, v = [kv rows, kv_heads, head_dim]; q_offsets = torch CUDA int32
-    [n + 1]; kv_offsets = the same for keys ([n] suffices with kv_lengths = [n]); status = torch CUDA int32 [1] or None."""
+    [n + 1]; kv_offsets = the same for keys ([n] suffices with kv_lengths = [n]); status = torch CUDA int32 [1], or None.
+
+    A sequence whose list is malformed, or leaves the buffers or the limits, is skipped and its rows of out stay as they were; nothing is raised, since the
+    lists are read on the device.  status tells once the stream has got there (0, PM_ERR_ARG or PM_ERR_TIMEOUT); without one operators_status() does.
+    Calls with few rows over long histories take a workspace from torch's allocator, on the call's stream: record them with torch.cuda.graph, whose
+    pool keeps it for the graph."""
     lib, where, (here, types) = load(), "pm_attention_packed", _start()
     t = _element_type(where, types, dtype)
     _on(where, "q", q, here, t)

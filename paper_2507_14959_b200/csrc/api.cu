@@ -1356,6 +1356,24 @@ int pm_layernorm(const void* x, const float* gamma, const float* beta, void* y, 
     return e == cudaSuccess ? PM_OK : PM_ERR_CUDA;
 }
 
+// pm_attention has no handle, hence no status word of its own: one word per device, allocated on first use
+static std::atomic<int*> attention_status[64];
+
+int pm_operators_status(void* cuda_stream) {
+    int dev = 0, found = 0;
+    if (const int rc = stream_device((cudaStream_t)cuda_stream, &dev); rc != PM_OK) return rc;
+    if (consumed(cudaStreamSynchronize((cudaStream_t)cuda_stream)) != cudaSuccess) return PM_ERR_CUDA;
+    int words[3] = {0, 0, 0};
+    if (consumed(packed_rows_take_status(&words[0])) != cudaSuccess || consumed(packed_tc_take_status(&words[1])) != cudaSuccess) return PM_ERR_CUDA;
+    if (int* word = dev < 64 ? attention_status[dev].load(std::memory_order_acquire) : nullptr) {
+        if (consumed(cudaMemcpy(&words[2], word, sizeof(int), cudaMemcpyDeviceToHost)) != cudaSuccess) return PM_ERR_CUDA;
+        if (words[2] != 0 && consumed(cudaMemset(word, 0, sizeof(int))) != cudaSuccess) return PM_ERR_CUDA;
+    }
+    for (int w : words)                                  // an expired wait before all else
+        if (found == 0 || w == PM_ERR_TIMEOUT) found = w;
+    return found;
+}
+
 int pm_attention(const void* qkv, void* out, int n_frames, int tokens, int heads, int dtype,
                  void* cuda_stream) {
     if (!qkv || !out || n_frames < 0 || tokens <= 0 || heads <= 0 || (dtype != 0 && dtype != 1))
@@ -1366,19 +1384,16 @@ int pm_attention(const void* qkv, void* out, int n_frames, int tokens, int heads
     if (dtype == 1) {
         e = launch_attention_simple<float>(L, (const float*)qkv, (float*)out, n_frames, tokens, heads);
     } else if (attention_tc_supported(tokens)) {
-        // the operator has no handle, hence no status word of its own: a bounded wait that expires is
-        // reported through the return code of a later call on the same device
-        // (one word per device, allocated on first use)
-        static std::atomic<int*> status_words[64];
+        // a bounded wait that expires is reported by pm_operators_status
         int dev = 0, n_sms = 0;
         if (consumed(cudaGetDevice(&dev)) != cudaSuccess || dev < 0 || dev >= 64 ||
             consumed(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return PM_ERR_CUDA;
-        int* status_word = status_words[dev].load(std::memory_order_acquire);
+        int* status_word = attention_status[dev].load(std::memory_order_acquire);
         if (!status_word) {
             if (consumed(cudaMalloc(&status_word, sizeof(int))) != cudaSuccess) return PM_ERR_OOM;
             if (consumed(cudaMemset(status_word, 0, sizeof(int))) != cudaSuccess) return PM_ERR_CUDA;
             int* expected = nullptr;
-            if (!status_words[dev].compare_exchange_strong(expected, status_word, std::memory_order_acq_rel)) {
+            if (!attention_status[dev].compare_exchange_strong(expected, status_word, std::memory_order_acq_rel)) {
                 cudaFree(status_word);                    // another thread got there first
                 status_word = expected;
             }

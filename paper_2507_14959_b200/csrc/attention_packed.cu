@@ -734,6 +734,8 @@ int packed_args(const pm_packed_attention* p, PackedArgs& a) {
 
 }  // namespace
 
+cudaError_t packed_rows_take_status(int* found) { return take_packed_status(found); }
+
 extern "C" {
 
 int pm_attention_packed_workspace(const pm_packed_attention* p, int n_sms, size_t* bytes) {

@@ -797,3 +797,5 @@ size_t packed_tc_workspace(const PackedArgs& a, int head_dim, int splits) {
 cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim, int n_sms, int splits, void* workspace) {
     return head_dim == 64 ? launch_tc<64>(L, a, n_sms, splits, workspace) : launch_tc<128>(L, a, n_sms, splits, workspace);
 }
+
+cudaError_t packed_tc_take_status(int* found) { return take_packed_status(found); }

@@ -23,8 +23,15 @@ cudaError_t launch_packed_tc(const Launch& L, const PackedArgs& a, int head_dim,
 
 namespace {
 
-// Where calls without a status word of their own leave what they find.
+// Where calls without a status word of their own leave what they find, until pm_operators_status reads it.  A word of each source file: its address
+// would have to be asked of the runtime, which a first call may not do while it is captured.
 __device__ int packed_status_word;
+cudaError_t take_packed_status(int* found) {
+    const int none = 0;
+    const cudaError_t e = consumed(cudaMemcpyFromSymbol(found, packed_status_word, sizeof(int)));
+    // kernels write to a word that is zero only, so none is lost in between
+    return e != cudaSuccess || *found == 0 ? e : consumed(cudaMemcpyToSymbol(packed_status_word, &none, sizeof(int)));
+}
 __device__ __forceinline__ int* packed_status(const PackedArgs& a) { return a.status ? a.status : &packed_status_word; }
 
 struct Segment { int q0, nq, k0, nk; };

@@ -50,3 +50,35 @@ def test_other_operators_after_a_call_that_failed():
         call(after)
         torch.cuda.synchronize()
         assert torch.equal(before, after) and before.abs().sum() > 0
+
+
+@pytest.mark.parametrize("dtype,queries,keys,form", [(0, 3, 40, ("16 rows", 1)), (0, 2000, 2000, ("tcgen05", 1)), (0, 2, 9000, ("16 rows", 2)), (0, 256, 8000, ("tcgen05", 2)),
+                                                     (1, 3, 40, ("fp32", 1)), (1, 70, 70, ("fp32", 1))])
+def test_skipped_sequences_are_reported_without_a_status_word(dtype, queries, keys, form):
+    from paper_2507_14959_b200 import binding
+    heads, kv_heads, dim = 8, 2, 128
+    t = (torch.bfloat16, torch.float32)[dtype]
+    took = binding.attention_packed_kernel(heads=heads, kv_heads=kv_heads, head_dim=dim, n_seqs=1, max_q=queries, max_kv=keys, dtype=dtype,
+                                           workspace_bytes=1 << 28 if form[1] > 1 else 0)
+    assert took[0] == form[0] and (took[2] > 1) == (form[1] > 1)
+    q, k, v = normal(1, queries, heads, dim).to(t).cuda(), normal(2, keys, kv_heads, dim).to(t).cuda(), normal(3, keys, kv_heads, dim).to(t).cuda()
+    q_off, k_off, good, bad, status = ints([0, queries]), ints([0]), ints([keys]), ints([keys + 1]), ints([0])
+    other = torch.cuda.Stream()
+
+    def call(lengths, **more):
+        out = torch.full_like(q, 7.0)
+        torch.cuda.synchronize()
+        binding.attention_packed(q, k, v, out, q_off, queries, keys, dtype, kv_offsets=k_off, kv_lengths=lengths, causal=True, **more)
+        return out
+    assert binding.operators_status() == 0
+    call(good)
+    assert binding.operators_status() == 0
+    for stream in (None, other):
+        out = call(bad, stream=stream)
+        assert binding.operators_status(stream) == binding.PM_ERR_ARG and (out == 7).all()
+        assert binding.operators_status(stream) == 0                       # taken away
+    call(bad)                                              # a call that goes well does not clear what an earlier one has left
+    call(good)
+    assert binding.operators_status() == binding.PM_ERR_ARG
+    call(bad, status=status)                               # a word of the caller's own is all that is written
+    assert binding.operators_status() == 0 and status.item() == binding.PM_ERR_ARG
