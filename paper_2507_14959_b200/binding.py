@@ -716,12 +716,12 @@ def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offset
         raise PolymorphError(rc, where)
 
 
-def attention_packed_kernel(*, heads, kv_heads, head_dim, n_seqs, max_q, max_kv, q_rows=None, kv_rows=None, dtype=0, workspace_bytes=0, n_sms=148):
+def attention_packed_kernel(*, heads, kv_heads, head_dim, n_seqs, max_q, max_kv, q_rows=None, kv_rows=None, causal=True, dtype=0, workspace_bytes=0, n_sms=148):
     """pm_attention_packed_kernel for a call of these sizes: ("16 rows", "tcgen05" or "fp32", CTAs of a cluster, CTAs through the workspace)."""
     q_rows, kv_rows = n_seqs * max_q if q_rows is None else q_rows, n_seqs * max_kv if kv_rows is None else kv_rows
     some = 1 << 20                                         # an aligned address; nothing is read
     args = _ATTENTION_ARGS.pack(some, some, some, some, heads * head_dim, kv_heads * head_dim, kv_heads * head_dim, heads * head_dim, some, some, 0, q_rows,
-                                kv_rows, n_seqs, max_q, max_kv, heads, kv_heads, head_dim, 1, 0.0, dtype, 0, some if workspace_bytes else 0, workspace_bytes)
+                                kv_rows, n_seqs, max_q, max_kv, heads, kv_heads, head_dim, 1 if causal else 0, 0.0, dtype, 0, some if workspace_bytes else 0, workspace_bytes)
     form = (C.c_int32 * 3)()
     rc = load().pm_attention_packed_kernel(args, n_sms, form)
     if rc != PM_OK:

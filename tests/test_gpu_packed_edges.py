@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_packed import bound, expected, ints, normal
+from test_gpu_packed import bound, check, expected, ints, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +82,24 @@ def test_skipped_sequences_are_reported_without_a_status_word(dtype, queries, ke
     assert binding.operators_status() == binding.PM_ERR_ARG
     call(bad, status=status)                               # a word of the caller's own is all that is written
     assert binding.operators_status() == 0 and status.item() == binding.PM_ERR_ARG
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads,lengths", [(128, 8, 2, [(256, 8000)]), (64, 4, 4, [(3000, 8192), (0, 500), (257, 0), (5, 5000)]), (64, 6, 2, [(700, 9000), (90, 300)]),
+                                                        (128, 2, 2, [(2000, 5000)])])
+def test_units_that_share_their_keys_without_causal_order(dim, heads, kv_heads, lengths):
+    from paper_2507_14959_b200 import binding
+    form = binding.attention_packed_kernel(heads=heads, kv_heads=kv_heads, head_dim=dim, n_seqs=len(lengths), max_q=max(a for a, _ in lengths), causal=False,
+                                           max_kv=max(b for _, b in lengths), q_rows=sum(a for a, _ in lengths) + 3, kv_rows=sum(b for _, b in lengths) + 3,
+                                           workspace_bytes=1 << 28)
+    assert form[0] == "tcgen05" and form[2] > 1, form
+    check(0, dim, heads, kv_heads, lengths, False, seed=73)
+
+
+@pytest.mark.parametrize("n,seqs,heads", [(300, 4, 8), (100, 16, 8), (1000, 1, 12)])
+def test_the_order_decides_the_kernel(n, seqs, heads):
+    """Of the same sizes the causal call takes tiles of 16 rows, the full one units of 256."""
+    from paper_2507_14959_b200 import binding
+    for causal, kernel in ((True, "16 rows"), (False, "tcgen05")):
+        assert binding.attention_packed_kernel(heads=heads, kv_heads=heads, head_dim=64, n_seqs=seqs, max_q=n, max_kv=n, q_rows=seqs * n + 3, kv_rows=seqs * n + 3,
+                                               causal=causal)[0] == kernel
+        check(0, 64, heads, heads, [(n, n)] * seqs, causal, packed=True, seed=74)
