@@ -411,7 +411,8 @@ typedef struct {
 } pm_rope_config;
 
 /* What the calls below take: filled by pm_rope_init on the host, plain data, copied by each call.  step[i] is pair i's
- * turns per position in units of 2^-64 turns, so angles of any 32-bit position are exact to 2^-33 turns. */
+ * turns per position in units of 2^-64 turns.  Angles of any 32-bit position are rounded to 2^-33 turns and, as floats, to 2^-24 of their distance
+ * from the nearest quarter turn (2^-28 turns at most): about half of the rounding of sine and cosine to 32 bits. */
 typedef struct {
     int head_dim, rot_dim, interleaved, axes;
     float amplitude;

@@ -4,9 +4,11 @@
 //     (a, b) -> (a cos t - b sin t, a sin t + b cos t)   for each pair (a, b) of u,  t = position * frequency of the pair
 //
 // Positions are whole numbers, so an angle is needed modulo one turn only: a frequency is held as the 64-bit fraction of a
-// turn per position, and the wrapped 64-bit product with the position is the angle's fraction of a turn, exact to 2^-33 turns
-// at any 32-bit position (a 32-bit product of position and frequency is off by 0.06 rad at position 10^6).  sincospi of that
-// fraction needs no argument reduction.
+// turn per position, and the wrapped 64-bit product with the position is the angle's fraction of a turn, to 2^-33 turns
+// at any 32-bit position (a 32-bit product of position and frequency is off by 0.06 rad at position 10^6).  It is rounded to
+// 32 bits, and the nearest quarter turn comes off before it becomes a float: at most an eighth of a turn is left, whose 24 bits are good
+// to 2^-28 turns, or 2^-24 of what is left (of a whole turn they would be good to 2^-26, which is more than the rounding of a sine in 32 bits).
+// Sine and cosine of the rest change places and signs with the quarter.
 //
 // Every element is read and written once.  A thread holds 16 elements of a head as 16-byte pieces (two of bf16, four of fp32) that lie
 // side by side with the neighbouring threads', so that each load and store of a warp covers whole lines: with half layout the pairs of the
@@ -169,10 +171,14 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_RESIDENT) rotate_kernel(const
 #pragma unroll
                 for (int i = 0; i < PPL; ++i) {
                     const long long p = a.positions[row * a.table.axes + axis[i]];
-                    const int turn = (int)(((unsigned long long)p * step[i]) >> 32);     // of 2^32 to a turn, signed
-                    sincospif((float)turn * 4.656612873077393e-10f, &ms[i], &mc[i]);     // 2^-31: in half turns
-                    mc[i] *= amplitude;
-                    ms[i] *= amplitude;
+                    const uint32_t turn = (uint32_t)(((unsigned long long)p * step[i] + 0x80000000ull) >> 32);     // of 2^32 to a turn
+                    const uint32_t quarter = (turn + 0x20000000u) >> 30;
+                    float sine, cosine;
+                    sincospif((float)(int)(turn - (quarter << 30)) * 4.656612873077393e-10f, &sine, &cosine);     // 2^-31: in half turns
+                    mc[i] = amplitude * (quarter & 1 ? sine : cosine);
+                    ms[i] = amplitude * (quarter & 1 ? cosine : sine);
+                    if ((quarter + 1) & 2) mc[i] = -mc[i];
+                    if (quarter & 2) ms[i] = -ms[i];
                 }
                 float fc[8], fs[8];
 #pragma unroll

@@ -103,3 +103,32 @@ def test_the_order_decides_the_kernel(n, seqs, heads):
         assert binding.attention_packed_kernel(heads=heads, kv_heads=heads, head_dim=64, n_seqs=seqs, max_q=n, max_kv=n, q_rows=seqs * n + 3, kv_rows=seqs * n + 3,
                                                causal=causal)[0] == kernel
         check(0, 64, heads, heads, [(n, n)] * seqs, causal, packed=True, seed=74)
+
+
+@pytest.mark.parametrize("dim,interleaved,axes", [(64, True, 1), (128, False, 1), (256, True, 2), (48, False, 2)])
+@pytest.mark.parametrize("far", [100, 10 ** 6, 2 ** 31 - 1])
+def test_angles_in_32_bits(dim, interleaved, axes, far):
+    """Sine and cosine themselves: every pair is (1, 0).  Against the wrapped 64-bit products of the positions and the table's steps."""
+    from paper_2507_14959_b200 import binding
+    rows = 3000
+    table = binding.RopeTable(dim, base=10000.0, interleaved=interleaved, axes=axes)
+    at = torch.randint(-far, far, (rows, axes), generator=torch.Generator().manual_seed(dim), dtype=torch.int64)
+    at[0], at[1] = far, 0
+    step = np.array(table.table.step[:dim // 2], dtype=np.uint64)
+    which = np.repeat(np.arange(axes), dim // 2 // axes)
+    fraction = at.numpy().astype(np.uint64)[:, which] * step                  # of 2^64 to a turn, wrapped
+    turns = torch.from_numpy((fraction >> np.uint64(11)).astype(np.float64) * 2.0 ** -53)
+    first, second = (slice(0, dim, 2), slice(1, dim, 2)) if interleaved else (slice(0, dim // 2), slice(dim // 2, dim))
+    x = torch.zeros((rows, 1, dim), device="cuda")
+    x[..., first] = 1
+    y = torch.zeros_like(x)
+    binding.rope(x, y, at.int().cuda() if axes == 2 else at[:, 0].int().cuda(), table, 1)
+    y = y[:, 0].cpu().double()
+    # the angle's rounding to 2^-33 turns; to a float, 2^-24 of its distance from the nearest quarter turn; sine and cosine to a unit of
+    # their last place, 2^-23 of them; the products with 1 and 0 are exact
+    rest = (turns - torch.round(turns * 4) / 4).abs() * 2 * np.pi
+    angle = 2 * np.pi * 2.0 ** -33 + 2.0 ** -24 * rest
+    for got, want in ((y[:, first], torch.cos(2 * np.pi * turns)), (y[:, second], torch.sin(2 * np.pi * turns))):
+        # (turns from 53 bits and the comparison's own roundings: 2^-50)
+        excess = (got - want).abs() - (angle + 2.0 ** -23 * want.abs() + 2.0 ** -50)
+        assert (excess <= 0).all(), excess.max()
