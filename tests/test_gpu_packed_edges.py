@@ -132,3 +132,39 @@ def test_angles_in_32_bits(dim, interleaved, axes, far):
         # (turns from 53 bits and the comparison's own roundings: 2^-50)
         excess = (got - want).abs() - (angle + 2.0 ** -23 * want.abs() + 2.0 ** -50)
         assert (excess <= 0).all(), excess.max()
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 1, 64), (16, 4, 128)])
+def test_many_streams_with_histories_of_every_length(heads, kv_heads, dim):
+    """More streams than a warp has lanes, in causal order; between the keys that their units see lie wide gaps."""
+    from paper_2507_14959_b200 import binding
+    lengths = [(n, n + kept) for n, kept in zip([300, 1, 40, 0, 129, 64, 600] * 11, [0, 9000, 3, 500, 0, 2000, 16, 0, 30000, 0, 700] * 7)]
+    form = binding.attention_packed_kernel(heads=heads, kv_heads=kv_heads, head_dim=dim, n_seqs=len(lengths), max_q=600, max_kv=max(b for _, b in lengths),
+                                           q_rows=sum(a for a, _ in lengths) + 3, kv_rows=sum(b for _, b in lengths) + 3)
+    assert form[0] == "tcgen05" and len(lengths) > 64
+    check(0, dim, heads, kv_heads, lengths, True, seed=75)
+
+
+def test_one_more_stream_costs_about_one_more_stream():
+    """A long history among short ones, with 32 streams and with 40: the search for the next unit does not go through all the keys between them."""
+    from paper_2507_14959_b200 import binding
+    heads, dim, new, kept = 64, 64, 16, 200000
+    times, cache = {}, torch.randn((kept + 40 * new, 1, dim), device="cuda").bfloat16()
+    for n in (32, 40):
+        q = normal(n, n * new, heads, dim).bfloat16().cuda()
+        out, q_off = torch.zeros_like(q), ints([i * new for i in range(n + 1)])
+        lengths = [kept] + [new] * (n - 1)
+        k_off, status = ints(np.cumsum([0] + lengths).tolist()), ints([0])
+        at = []
+        for _ in range(7):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            binding.attention_packed(q, cache, cache, out, q_off, new, kept, 0, kv_offsets=k_off, causal=True, status=status)
+            end.record()
+            torch.cuda.synchronize()
+            at.append(start.elapsed_time(end))
+        times[n] = sorted(at)[3]
+        assert status.item() == 0
+        want, mean, size = expected(q[:new], cache[:kept], cache[:kept], True, dim ** -0.5)
+        assert ((out[:new].double() - want).abs() <= bound(0, want, mean, size, dim, kept)).all()
+    assert times[40] < 3 * times[32], times               # level by level of 4 keys it was 20 times as long
