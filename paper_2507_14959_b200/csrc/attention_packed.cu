@@ -574,6 +574,15 @@ __global__ void __launch_bounds__(256, 2) attention_f32_kernel(const __grid_cons
     }
 }
 
+// The lists of a call that leaves no row to attend (max_q or q_rows 0): sequences that have queries all the same, or are malformed, are reported as by
+// the other kernels.
+__global__ void check_lists_kernel(const __grid_constant__ PackedArgs a) {
+    dep_release();
+    dep_wait();
+    const int s = blockIdx.x * blockDim.x + threadIdx.x;
+    if (s < a.n_seqs) packed_segment(a, s);
+}
+
 // CTAs that share the keys of a row tile: while the grid leaves room for them and each still has `least` keys; and of long histories, whose
 // lengths may differ, up to eight times as many CTAs as run at once, each with `even` keys still, so that they end together (48 streams of
 // up to 8192 keys: 133 us with a CTA each, 126 with two, 118 with four)
@@ -706,7 +715,7 @@ bool bf16_form(const PackedArgs& a, int head_dim, int n_sms, size_t bytes, RowsF
     return rows_time(a, head_dim, f, n_sms) < tc_time(a, head_dim, splits, n_sms);
 }
 
-// Checks everything the host can see; PM_OK with nothing to do leaves a.n_seqs 0.
+// Checks everything the host can see; PM_OK with nothing to attend leaves a.heads 0, and a.n_seqs is then the number of lists to check.
 int packed_args(const pm_packed_attention* p, PackedArgs& a) {
     if (!p || p->q_rows < 0 || p->kv_rows < 0 || p->n_seqs < 0 || p->max_q < 0 || p->max_kv < 0 || p->heads <= 0 || p->kv_heads <= 0 ||
         p->heads % p->kv_heads || (p->head_dim != 64 && p->head_dim != 128) || (p->dtype != 0 && p->dtype != 1) || !(p->scale >= 0.f) || !isfinite(p->scale))
@@ -715,7 +724,14 @@ int packed_args(const pm_packed_attention* p, PackedArgs& a) {
         (long long)std::min(p->max_q, p->q_rows) * (p->heads / p->kv_heads) > INT32_MAX / 2)
         return PM_ERR_CAPACITY;
     a = PackedArgs{};
-    if (p->n_seqs == 0 || p->q_rows == 0 || p->max_q == 0) return PM_OK;
+    a.q_offsets = p->q_offsets; a.kv_offsets = p->kv_offsets; a.kv_lengths = p->kv_lengths;
+    a.q_rows = p->q_rows; a.kv_rows = p->kv_rows;
+    a.max_q = std::min(p->max_q, p->q_rows); a.max_kv = std::min(p->max_kv, p->kv_rows);
+    if (p->n_seqs == 0 || a.max_q == 0) {
+        if (p->q_offsets && (p->kv_offsets || !p->kv_lengths)) a.n_seqs = p->n_seqs;
+        return PM_OK;
+    }
+    a.n_seqs = p->n_seqs;
     if (!heads_ok(p->q, p->q_stride, p->heads, p->head_dim, p->dtype) || !heads_ok(p->out, p->out_stride, p->heads, p->head_dim, p->dtype) ||
         !p->q_offsets || (p->kv_lengths && !p->kv_offsets) || ((uintptr_t)p->workspace & 31))
         return PM_ERR_ARG;
@@ -724,9 +740,6 @@ int packed_args(const pm_packed_attention* p, PackedArgs& a) {
         return PM_ERR_ARG;
     a.q = p->q; a.k = p->k; a.v = p->v; a.out = p->out;
     a.q_stride = p->q_stride; a.k_stride = p->k_stride; a.v_stride = p->v_stride; a.out_stride = p->out_stride;
-    a.q_offsets = p->q_offsets; a.kv_offsets = p->kv_offsets; a.kv_lengths = p->kv_lengths;
-    a.q_rows = p->q_rows; a.kv_rows = p->kv_rows; a.n_seqs = p->n_seqs;
-    a.max_q = std::min(p->max_q, p->q_rows); a.max_kv = std::min(p->max_kv, p->kv_rows);
     a.heads = p->heads; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads; a.causal = p->causal != 0;
     a.c = (p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
     return PM_OK;
@@ -743,7 +756,7 @@ int pm_attention_packed_workspace(const pm_packed_attention* p, int n_sms, size_
     if (!bytes || n_sms <= 0) return PM_ERR_ARG;
     if (const int rc = packed_args(p, a); rc != PM_OK) return rc;
     *bytes = 0;
-    if (a.n_seqs > 0 && p->dtype == 0) {
+    if (a.heads > 0 && p->dtype == 0) {
         RowsForm f;
         int splits;
         *bytes = bf16_form(a, p->head_dim, n_sms, SIZE_MAX, f, splits) ? rows_workspace(a, p->head_dim, f) : packed_tc_workspace(a, p->head_dim, splits);
@@ -756,7 +769,7 @@ int pm_attention_packed_kernel(const pm_packed_attention* p, int n_sms, int32_t*
     if (!form || n_sms <= 0) return PM_ERR_ARG;
     if (const int rc = packed_args(p, a); rc != PM_OK) return rc;
     form[0] = -1; form[1] = form[2] = 1;
-    if (a.n_seqs == 0) return PM_OK;
+    if (a.heads == 0) return PM_OK;
     if (p->dtype == 1) {
         const F32Form f = f32_form(a, n_sms);
         form[0] = 2; form[1] = f.cluster;
@@ -779,12 +792,15 @@ int pm_attention_packed(const pm_packed_attention* p, void* cuda_stream) {
     int dev = 0, n_sms = 0;
     if (const int rc = stream_device(st, &dev); rc != PM_OK) return rc;
     if (p->status_out && consumed(cudaMemsetAsync(p->status_out, 0, sizeof(int32_t), st)) != cudaSuccess) return PM_ERR_CUDA;
-    if (a.n_seqs == 0) return PM_OK;
-    if (consumed(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return PM_ERR_CUDA;
     a.status = p->status_out;
     Launch L;
     L.st = st;
     L.status = a.status;
+    if (a.heads == 0) {
+        if (a.n_seqs == 0) return PM_OK;
+        return launch_overlapped(L, check_lists_kernel, (a.n_seqs + 127) / 128, 128, 0, 1, a) == cudaSuccess ? PM_OK : PM_ERR_CUDA;
+    }
+    if (consumed(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return PM_ERR_CUDA;
     cudaError_t e;
     RowsForm f;
     int splits = 1;

@@ -168,3 +168,24 @@ def test_one_more_stream_costs_about_one_more_stream():
         want, mean, size = expected(q[:new], cache[:kept], cache[:kept], True, dim ** -0.5)
         assert ((out[:new].double() - want).abs() <= bound(0, want, mean, size, dim, kept)).all()
     assert times[40] < 3 * times[32], times               # level by level of 4 keys it was 20 times as long
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_lists_of_a_call_without_rows_are_checked(dtype):
+    """A limit, or a buffer, of no queries: sequences that have some are reported, whatever else is in order; nothing is written."""
+    from paper_2507_14959_b200 import binding
+    t = (torch.bfloat16, torch.float32)[dtype]
+    q, empty = torch.ones((8, 2, 64), dtype=t, device="cuda"), torch.ones((0, 2, 64), dtype=t, device="cuda")
+    out, status = torch.full_like(q, 7.0), ints([9])
+
+    def call(rows, q_offsets, max_q, **keys):
+        binding.attention_packed(rows, q, q, out[:len(rows)], ints(q_offsets), max_q, 8, dtype, status=status, **{n: ints(v) for n, v in keys.items()})
+        return status.item()
+    for rows, max_q in ((q, 0), (empty, 0), (empty, 5)):
+        assert call(rows, [0, 0, 0], max_q) == 0
+        assert call(rows, [0, 4, 4], max_q) == binding.PM_ERR_ARG
+        assert call(rows, [0, 0, 0], max_q, kv_offsets=[0, 4, 8]) == 0
+        assert call(rows, [0, 0, 0], max_q, kv_offsets=[0, 4, 9]) == binding.PM_ERR_ARG
+        assert call(rows, [0] * 301, max_q, kv_offsets=[0] * 300, kv_lengths=[0] * 299 + [-1]) == binding.PM_ERR_ARG
+        assert call(rows, [0], max_q) == 0
+    assert (out == 7).all()
