@@ -475,7 +475,7 @@ typedef struct {
     int heads, kv_heads;                  /* heads a multiple of kv_heads, at most PM_PACKED_MAX_GROUP times   */
     int head_dim;                         /* 64 or 128                                                         */
     int causal;
-    float scale;                          /* > 0, or 0 for 1 / sqrt(head_dim)                                  */
+    float scale;                          /* > 0, or 0 for 1 / sqrt(head_dim); scale * log2(e) is finite           */
     int dtype;                            /* 0 = bf16 tensor-core kernels, 1 = fp32                            */
     int32_t* status_out;                  /* dev int32, cleared by the call, or NULL: pm_operators_status tells.  PM_ERR_ARG if a sequence's offsets
                                              or length are malformed, lie outside the buffers or exceed max_q / max_kv (the sequence is skipped,

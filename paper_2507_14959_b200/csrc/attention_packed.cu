@@ -715,10 +715,13 @@ bool bf16_form(const PackedArgs& a, int head_dim, int n_sms, size_t bytes, RowsF
     return rows_time(a, head_dim, f, n_sms) < tc_time(a, head_dim, splits, n_sms);
 }
 
+// scores are taken to powers of two
+constexpr float LOG2E = 1.4426950408889634f;
+
 // Checks everything the host can see; PM_OK with nothing to attend leaves a.heads 0, and a.n_seqs is then the number of lists to check.
 int packed_args(const pm_packed_attention* p, PackedArgs& a) {
     if (!p || p->q_rows < 0 || p->kv_rows < 0 || p->n_seqs < 0 || p->max_q < 0 || p->max_kv < 0 || p->heads <= 0 || p->kv_heads <= 0 ||
-        p->heads % p->kv_heads || (p->head_dim != 64 && p->head_dim != 128) || (p->dtype != 0 && p->dtype != 1) || !(p->scale >= 0.f) || !isfinite(p->scale))
+        p->heads % p->kv_heads || (p->head_dim != 64 && p->head_dim != 128) || (p->dtype != 0 && p->dtype != 1) || !(p->scale >= 0.f) || !isfinite(p->scale * LOG2E))
         return PM_ERR_ARG;
     if (p->n_seqs > PM_PACKED_MAX_SEQS || p->heads / p->kv_heads > PM_PACKED_MAX_GROUP || p->kv_heads > 65535 ||
         (long long)std::min(p->max_q, p->q_rows) * (p->heads / p->kv_heads) > INT32_MAX / 2)
@@ -741,7 +744,7 @@ int packed_args(const pm_packed_attention* p, PackedArgs& a) {
     a.q = p->q; a.k = p->k; a.v = p->v; a.out = p->out;
     a.q_stride = p->q_stride; a.k_stride = p->k_stride; a.v_stride = p->v_stride; a.out_stride = p->out_stride;
     a.heads = p->heads; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads; a.causal = p->causal != 0;
-    a.c = (p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
+    a.c = (p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->head_dim)) * LOG2E;
     return PM_OK;
 }
 

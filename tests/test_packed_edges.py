@@ -31,3 +31,15 @@ def test_the_kernel_of_a_call_is_told_for_its_own_order(lib, sizes):
         told.append(binding.attention_packed_kernel(**sizes, causal=causal))
         assert told[-1] == (("16 rows", "tcgen05", "fp32")[form[0]], form[1], form[2])
     assert told[0] != told[1]
+
+
+@pytest.mark.parametrize("scale,refused", [(2.3e38, False), (2.4e38, True), (3.4e38, True)])
+def test_a_scale_whose_exponent_of_two_overflows_is_refused(lib, scale, refused):
+    """Times log2(e) it would be infinite, and products that are zero would come out as no numbers."""
+    some = {n: 1 << 20 for n in ("q", "k", "v", "out", "q_offsets")}
+    args = binding.pm_packed_attention(**some, q_stride=128, k_stride=128, v_stride=128, out_stride=128, q_rows=8, kv_rows=8, n_seqs=1, max_q=8, max_kv=8,
+                                       heads=2, kv_heads=2, head_dim=64, scale=scale)
+    form = (C.c_int32 * 3)()
+    assert lib.pm_attention_packed_kernel(C.byref(args), 148, form) == (binding.PM_ERR_ARG if refused else 0)
+    if refused:
+        assert lib.pm_attention_packed(C.byref(args), None) == binding.PM_ERR_ARG
