@@ -514,7 +514,9 @@ def _refuse(where, detail):
 
 
 def _on(where, name, t, here, dtype):
-    """Refuses a tensor of another element type, on the host or on another device than the current one."""
+    """Refuses a tensor that is missing, of another element type, on the host or on another device than the current one."""
+    if t is None:
+        _refuse(where, f"{name} is missing")
     if t.get_device() != here or here is None:
         _refuse(where, f"{name} is not on the current device")
     if t.dtype is not dtype:
@@ -567,9 +569,12 @@ class RopeTable:
 
 
 def _positions(where, positions, rows, axes, here):
+    _on(where, "positions", positions, here, _int32)
     if positions.shape != ((rows,) if axes == 1 else (rows, 2)) and positions.shape != (rows, axes):
         _refuse(where, f"positions has shape {tuple(positions.shape)}")
-    return _indexes(where, "positions", positions, here, rows * axes)
+    if not positions.is_contiguous():
+        _refuse(where, "positions is not contiguous")
+    return positions.data_ptr()
 
 
 def rope(x, y, positions, table, dtype, stream=None):
@@ -624,7 +629,7 @@ def qk_norm_rope(q, k, q_out, k_out, q_gamma, k_gamma, *, norm, eps, dtype, q_be
     _on(where, "q_out", q_out, here, t)
     rows, heads, dim, qs = _heads(where, "q", q)
     q_shape = _heads(where, "q_out", q_out)
-    per_head = q_gamma.dim() == 2
+    per_head = q_gamma is not None and q_gamma.dim() == 2
     kv_heads = ks = kos = kp = kop = 0
     if k is not None:
         _on(where, "k", k, here, t)
@@ -693,7 +698,7 @@ def attention_packed(q, k, v, out, q_offsets, max_q, max_kv, dtype, *, kv_offset
         _refuse(where, "shapes differ")
     if scale is not None and not scale > 0:
         _refuse(where, "scale is positive")
-    n = q_offsets.numel() - 1
+    n = -1 if q_offsets is None else q_offsets.numel() - 1
     qo, ko, kl, sp = _indexes(where, "q_offsets", q_offsets, here, n + 1), 0, 0, 0
     if kv_lengths is not None:
         kl = _indexes(where, "kv_lengths", kv_lengths, here, n)

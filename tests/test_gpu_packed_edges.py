@@ -189,3 +189,19 @@ def test_lists_of_a_call_without_rows_are_checked(dtype):
         assert call(rows, [0] * 301, max_q, kv_offsets=[0] * 300, kv_lengths=[0] * 299 + [-1]) == binding.PM_ERR_ARG
         assert call(rows, [0], max_q) == 0
     assert (out == 7).all()
+
+
+def test_missing_tensors_are_refused():
+    from paper_2507_14959_b200 import binding
+    x, off, gamma, table = torch.zeros((4, 2, 64), dtype=torch.bfloat16, device="cuda"), ints([0, 4]), torch.ones(64, device="cuda"), binding.RopeTable(64)
+    norm = lambda *a, **k: binding.qk_norm_rope(*a, norm="rms", eps=1e-6, dtype=0, **k)  # noqa: E731
+    calls = [lambda i=i: binding.attention_packed(*[None if j == i else t for j, t in enumerate((x, x, x, x))], off, 4, 4, 0) for i in range(4)]
+    calls += [lambda: binding.attention_packed(x, x, x, x, None, 4, 4, 0), lambda: binding.attention_packed(x, x, x, x, ints([]), 4, 4, 0)]
+    calls += [lambda: binding.rope(None, x, off, table, 0), lambda: binding.rope(x, None, off, table, 0), lambda: binding.rope(x, x, None, table, 0),
+              lambda: norm(None, x, x, x, gamma, gamma), lambda: norm(x, x, None, x, gamma, gamma), lambda: norm(x, x, x, None, gamma, gamma),
+              lambda: norm(x, x, x, x, None, gamma), lambda: norm(x, x, x, x, gamma, None), lambda: norm(x, x, x, x, gamma, gamma, table=table),
+              lambda: norm(x, x, x, x, gamma, gamma, positions=off)]
+    for i, call in enumerate(calls):
+        with pytest.raises(binding.PolymorphError) as e:
+            call()
+        assert e.value.code == binding.PM_ERR_ARG, i
