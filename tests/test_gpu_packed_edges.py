@@ -205,3 +205,65 @@ def test_missing_tensors_are_refused():
         with pytest.raises(binding.PolymorphError) as e:
             call()
         assert e.value.code == binding.PM_ERR_ARG, i
+
+
+def test_first_calls_in_32_bits_may_be_captured():
+    """As in 16 bits: nothing is set up by a first call that a capture could not hold, and the replay computes what an eager call does."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2507_14959_b200 import binding
+ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+x = torch.randn(600, 8, 64, device="cuda")
+table, at, g1 = binding.RopeTable(64), ints(list(range(600))), torch.ones(64, device="cuda")
+few, all_, hist = ints([0, 3]), ints([0, 100, 600]), ints([0, 600])
+def calls(o):
+    binding.rope(x, o[0], at, table, 1)
+    binding.qk_norm_rope(x, None, o[1], None, g1, None, norm="layer", eps=1e-6, dtype=1, positions=at, table=table)
+    binding.attention_packed(x, x, x, o[2], few, 3, 600, 1, kv_offsets=hist, causal=True)
+    binding.attention_packed(x, x, x, o[3], all_, 500, 500, 1)
+outs, eager = ([torch.zeros_like(x) for _ in range(4)] for _ in range(2))
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls(outs)
+assert all(o.abs().sum() == 0 for o in outs)
+graph.replay()
+torch.cuda.synchronize()
+calls(eager)
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) and a[:3].abs().sum() > 0 for a, b in zip(outs, eager))
+assert all(o[599].abs().sum() > 0 for o in (outs[0], outs[1], outs[3])) and outs[2][3:].abs().sum() == 0
+print("captured")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "captured" in done.stdout, done.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lengths,form", [([(1, 9000)], ("16 rows", True)), ([(256, 8000)], ("tcgen05", True)), ([(300, 300), (1000, 1000), (5, 700)] * 4, ("tcgen05", False)),
+                                          ([(40, 40), (3, 500)], ("16 rows", False))])
+def test_the_same_call_gives_the_same_bits(lengths, form, dim):
+    """Every form, with other work in between: no sum's order depends on the run."""
+    from paper_2507_14959_b200 import binding
+    heads, kv_heads = 8, 2
+    n_q, n_k = [a for a, _ in lengths], [b for _, b in lengths]
+    took = binding.attention_packed_kernel(heads=heads, kv_heads=kv_heads, head_dim=dim, n_seqs=len(lengths), max_q=max(n_q), max_kv=max(n_k), q_rows=sum(n_q),
+                                           kv_rows=sum(n_k), workspace_bytes=1 << 28)
+    assert (took[0], took[2] > 1) == form, took
+    q, k, v = (normal(i, n, h, dim).bfloat16().cuda() for i, n, h in ((1, sum(n_q), heads), (2, sum(n_k), kv_heads), (3, sum(n_k), kv_heads)))
+    q_off, k_off, first = ints(np.cumsum([0] + n_q).tolist()), ints(np.cumsum([0] + n_k).tolist()), None
+    noise, other = torch.randn(2048, 2048, device="cuda"), torch.cuda.Stream()
+    for turn in range(8):
+        out = torch.full_like(q, 7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            for _ in range(turn):
+                noise @ noise
+        binding.attention_packed(q, k, v, out, q_off, max(n_q), max(n_k), 0, kv_offsets=k_off, causal=True)
+        torch.cuda.synchronize()
+        first = out if first is None else first
+        assert torch.equal(first, out)
