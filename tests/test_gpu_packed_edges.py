@@ -267,3 +267,16 @@ def test_the_same_call_gives_the_same_bits(lengths, form, dim):
         torch.cuda.synchronize()
         first = out if first is None else first
         assert torch.equal(first, out)
+
+
+def test_smoke_takes_no_cooperative_launch(capsys, monkeypatch):
+    """smoke() is run under a profiler too, which the whole-network kernel's cooperative launch of clusters does not survive."""
+    import __graft_entry__
+    from paper_2507_14959_b200 import binding
+    switched = []
+    turn = binding.Model.set_small_batch_kernel
+    monkeypatch.setattr(binding.Model, "set_small_batch_kernel", lambda m, on: (switched.append(bool(on)), turn(m, on))[1])
+    __graft_entry__.smoke()
+    said = capsys.readouterr().out
+    # the whole-network kernel is one launch for the forward, the selection another
+    assert switched == [False] and int(said.split("launches ")[1].split()[0]) > 20 and "packed sequences" in said
