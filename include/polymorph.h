@@ -478,7 +478,7 @@ typedef struct {
     float scale;                          /* > 0, or 0 for 1 / sqrt(head_dim); scale * log2(e) is finite           */
     int dtype;                            /* 0 = bf16 tensor-core kernels, 1 = fp32                            */
     int32_t* status_out;                  /* dev int32, cleared by the call, or NULL: pm_operators_status tells.  PM_ERR_ARG if a sequence's offsets
-                                             or length are malformed, lie outside the buffers or exceed max_q / max_kv (the sequence is skipped,
+                                             or length are malformed, lie outside the buffers or exceed max_q, max_kv or PM_PACKED_MAX_KEYS (the sequence is skipped,
                                              its rows of out left as they were), PM_ERR_TIMEOUT if a bounded wait expired (rows of out are then
                                              undefined) */
     void* workspace;                      /* dev, 32-byte aligned, or NULL; see pm_attention_packed_workspace  */
@@ -487,6 +487,7 @@ typedef struct {
 
 #define PM_PACKED_MAX_SEQS 4096
 #define PM_PACKED_MAX_GROUP 64
+#define PM_PACKED_MAX_KEYS (1 << 24)      /* of a sequence; one with more is skipped, PM_ERR_ARG in its status: sums in 32 bits take no more terms */
 /* Errors: PM_ERR_ARG (NULL, ranges, alignment), PM_ERR_CAPACITY (n_seqs, heads / kv_heads, kv_heads > 65535, max_q * heads / kv_heads >= 2^30),
  * PM_ERR_CUDA.  Nothing is launched on the first two; with PM_ERR_CUDA a part of the call may have been, and out is then not complete. */
 int pm_attention_packed(const pm_packed_attention* args, void* cuda_stream);

@@ -729,7 +729,10 @@ int packed_args(const pm_packed_attention* p, PackedArgs& a) {
     a = PackedArgs{};
     a.q_offsets = p->q_offsets; a.kv_offsets = p->kv_offsets; a.kv_lengths = p->kv_lengths;
     a.q_rows = p->q_rows; a.kv_rows = p->kv_rows;
-    a.max_q = std::min(p->max_q, p->q_rows); a.max_kv = std::min(p->max_kv, p->kv_rows);
+    a.max_q = std::min(p->max_q, p->q_rows);
+    // Equal weights of 1 add up exactly in 32 bits to 2^24 terms and not at all from there on.  (And a unit of 2^27 keys would take longer than the bounded
+    // waits allow: 0.76 us per 64.)
+    a.max_kv = std::min({p->max_kv, p->kv_rows, PM_PACKED_MAX_KEYS});
     if (p->n_seqs == 0 || a.max_q == 0) {
         if (p->q_offsets && (p->kv_offsets || !p->kv_lengths)) a.n_seqs = p->n_seqs;
         return PM_OK;

@@ -280,3 +280,20 @@ def test_smoke_takes_no_cooperative_launch(capsys, monkeypatch):
     said = capsys.readouterr().out
     # the whole-network kernel is one launch for the forward, the selection another
     assert switched == [False] and int(said.split("launches ")[1].split()[0]) > 20 and "packed sequences" in said
+
+
+@pytest.mark.parametrize("dtype,queries,kernel", [(0, 1, "16 rows"), (0, 300, "tcgen05"), (1, 2, "fp32")])
+def test_the_longest_history(dtype, queries, kernel):
+    """2^24 equal weights add up exactly, whatever their order; a longer history is not served."""
+    from paper_2507_14959_b200 import binding
+    t, n, dim = (torch.bfloat16, torch.float32)[dtype], 1 << 24, 64
+    form = binding.attention_packed_kernel(heads=8, kv_heads=1, head_dim=dim, n_seqs=1, max_q=queries, max_kv=2 ** 31 - 1, kv_rows=n + 1, dtype=dtype,
+                                           workspace_bytes=1 << 28)
+    assert form[0] == kernel
+    q, k, v = normal(1, queries, 8, dim).to(t).cuda(), torch.zeros((n + 1, 1, dim), dtype=t, device="cuda"), torch.ones((n + 1, 1, dim), dtype=t, device="cuda")
+    for keys in (n, n + 1):
+        out, status = torch.full_like(q, 7.0), ints([5])
+        binding.attention_packed(q, k, v, out, ints([0, queries]), queries, 2 ** 31 - 1, dtype, kv_offsets=ints([0]), kv_lengths=ints([keys]), causal=True,
+                                 status=status)
+        assert status.item() == (0 if keys == n else binding.PM_ERR_ARG)
+        assert (out == (1 if keys == n else 7)).all()
