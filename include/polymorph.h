@@ -411,7 +411,8 @@ typedef struct {
 } pm_rope_config;
 
 /* What the calls below take: filled by pm_rope_init on the host, plain data, copied by each call.  step[i] is pair i's
- * turns per position in units of 2^-64 turns.  Angles of any 32-bit position are rounded to 2^-33 turns and, as floats, to 2^-24 of their distance
+ * turns per position in units of 2^-64 turns (a base or factor far below 1 can give frequencies of 2^k turns a position, of whose fraction 64 - k bits are
+ * known; from 2^64 on the pair is not turned).  Angles of any 32-bit position are rounded to 2^-33 turns and, as floats, to 2^-24 of their distance
  * from the nearest quarter turn (2^-28 turns at most): about half of the rounding of sine and cosine to 32 bits. */
 typedef struct {
     int head_dim, rot_dim, interleaved, axes;
@@ -420,7 +421,7 @@ typedef struct {
     unsigned long long step[PM_ROPE_MAX_DIM / 2];
 } pm_rope_table;
 
-/* Host function; needs no GPU.  Errors: PM_ERR_ARG (NULL, a value out of the ranges above, frequencies that overflow),
+/* Host function; needs no GPU.  Errors: PM_ERR_ARG (NULL, a value out of the ranges above, frequencies that the host's long double does not hold),
  * PM_ERR_CAPACITY (head_dim > PM_ROPE_MAX_DIM). */
 int pm_rope_init(const pm_rope_config* cfg, pm_rope_table* out);
 
@@ -476,7 +477,8 @@ typedef struct {
     int head_dim;                         /* 64 or 128                                                         */
     int causal;
     float scale;                          /* > 0, or 0 for 1 / sqrt(head_dim); scale * log2(e) is finite           */
-    int dtype;                            /* 0 = bf16 tensor-core kernels, 1 = fp32                            */
+    int dtype;                            /* 0 = bf16 tensor-core kernels: weights are rounded to bf16 for the product with v (2^-8 of each), and in
+                                             calls of many rows a quarter of the exponentials is good to 2^-13.7; 1 = fp32 throughout */
     int32_t* status_out;                  /* dev int32, cleared by the call, or NULL: pm_operators_status tells.  PM_ERR_ARG if a sequence's offsets
                                              or length are malformed, lie outside the buffers or exceed max_q, max_kv or PM_PACKED_MAX_KEYS (the sequence is skipped,
                                              its rows of out left as they were), PM_ERR_TIMEOUT if a bounded wait expired (rows of out are then

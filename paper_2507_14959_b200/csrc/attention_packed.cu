@@ -622,7 +622,8 @@ RowsForm rows_form(const PackedArgs& a, int n_sms, bool workspace) {
     return f;
 }
 // What both kernels take, in us, as measured on a B200 (twenty shapes of 1 to 256 sequences, 16 to 1024 rows per K/V head and 17 to 16000 keys:
-// within a third of either kernel's time, and the faster one is chosen in every one of them).
+// within a third of either kernel's time, and the faster one is chosen in every one of them).  Units of uneven length are taken for even ones: 985 to 250 new
+// tokens of four streams over up to 4985 keys, 12 / 4 heads of 64, are 66 here and 55 with their keys cut in two, and take 77 either way.
 //   16-row tiles:  3, joining 2 (4 through a workspace), 0.001 for a CTA without a tile; one with a tile 0.55 and per 16 keys 0.07 (head dim 64)
 //                  or 0.15 (128) beside another on its multiprocessor, 1.6 times that alone
 //   tcgen05:       5, joining 4 and what the parts take at 4 TB/s; a unit of 256 rows 1.3 and per block of 64 keys 0.76, whatever its rows: two
@@ -700,10 +701,6 @@ cudaError_t launch_f32(const Launch& L, const PackedArgs& a, const F32Form& f) {
 bool heads_ok(const void* p, long long stride, int heads, int dim, int dtype) {
     return p && ((uintptr_t)p & 15) == 0 && stride >= (long long)heads * dim && stride % (dtype == 0 ? 8 : 4) == 0;
 }
-
-}  // namespace
-
-namespace {
 
 // Whether 16-row tiles serve a bf16 call with that much workspace; their form, and the units that share keys otherwise.
 bool bf16_form(const PackedArgs& a, int head_dim, int n_sms, size_t bytes, RowsForm& f, int& splits) {

@@ -146,8 +146,8 @@ bool attention_encode_maps(const bf16* qkv, int n_frames, int tokens, int heads,
 // n_sms > 0 selects the pipelined persistent kernel where it applies (one key block); 0 = never
 cudaError_t launch_attention_tc(const Launch& L, const CUtensorMap& tm_q, const CUtensorMap& tm_kv,
                                 const bf16* qkv, bf16* out, int n_frames, int tokens, int heads, int n_sms);
-// attention over packed sequences: what calls without a status word of their own have left on the current device since the last time (0: nothing), taken away: of the kernels
-// in attention_packed.cu, in attention_packed_tc.cu.  Synchronous.
+// Attention over packed sequences: what calls without a status word of their own have left on the current device since the last time (0: nothing),
+// taken away: of the kernels in attention_packed.cu, in attention_packed_tc.cu.  Synchronous.
 cudaError_t packed_rows_take_status(int* found);
 cudaError_t packed_tc_take_status(int* found);
 // patch gather, and the CLS rows of x
